@@ -132,6 +132,24 @@ int ob_varlen_attn_bwd_static(const void *d_o, const void *q, const void *k, con
                               const ob_segments *seg, int nq, int nkv, int d, float scale, int mask,
                               int dtype, void *hip_stream);
 
+/* ---- varlen attention with a sliding window and sinks ------------------------------------------
+ * As above, causal, with allowed(i, j) <=> same segment, j <= i, and (i - j < window or j is one of the segment's first
+ * `sinks` tokens).  window >= 1 (a row sees itself: none is empty; a window as long as the segments is plain causal
+ * attention), 0 <= sinks <= 64, scale > 0; row strides up to 2^24 elements, tensors and workspace aligned to 16 bytes.  Key
+ * tiles that no row of a workgroup sees are not computed, so a call costs tokens * window, not tokens^2.  Nothing of another segment is
+ * read on a segment's behalf; inside a segment an infinity or NaN in a row of k, v or d_o may also reach rows near it that do not see it.
+ * The backward's workspace (ob_varlen_attn_window_bwd_workspace_bytes for the same arguments; 0 if they are refused) holds the
+ * row statistics and, for the sinks of segments longer than the window, the fp32 sums over chunks of their queries, which are
+ * added in order: no atomics, results are bitwise reproducible. */
+int ob_varlen_attn_window_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
+                              const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, int dtype,
+                              void *hip_stream);
+size_t ob_varlen_attn_window_bwd_workspace_bytes(const ob_segments *seg, int nq, int nkv, int d, int window, int sinks, int dtype);
+int ob_varlen_attn_window_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
+                              void *dq, void *dk, void *dv, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
+                              int nkv, int d, float scale, int window, int sinks, int dtype, void *ws, size_t ws_bytes,
+                              void *hip_stream);
+
 /* ---- one transformer block (steps a1..a9 / b9..b1) -------------------------------------------
  * ob_block_fwd:  y = Block(x); keeps in `saved` (ob_block_saved_bytes) what the backward needs.
  * ob_block_bwd:  given dy, the same x, weights and `saved`, writes dx and every weight gradient
@@ -245,6 +263,28 @@ int ob_connector_bwd(const ob_connector_desc *desc, const ob_connector_weights *
                      void *dv, int n_tiles, const int32_t *dst_rows_host,
                      const int32_t *dst_rows_dev, int llm_tokens, const void *saved,
                      size_t saved_bytes, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* ---- rotary positions with several axes ---------------------------------------------------------
+ * The blocks above turn by a token's distance to the start of its segment.  Image and video tokens have a place along several
+ * axes (time, height, width): here pair i of a head, its elements (i, i + d/2), turns by a = pos[axis_of_pair[i]][t] theta_i:
+ *   y_i = x_i cos a - x_{i+d/2} sin a,   y_{i+d/2} = x_{i+d/2} cos a + x_i sin a
+ * axis_of_pair[i] = -1: the pair passes as it is.  theta_i = base^(-2i/d), one spectrum over the head, or with per_axis
+ * base^(-j/n) for the j-th of the n pairs of its axis, a spectrum for each.  Runs of pairs, axes in turns, a part of the
+ * head: all a choice of axis_of_pair.  inverse != 0 turns back: the gradient of x from that of y.
+ * x: rows of n_heads heads of head_dim elements at row stride ldx, y at ldy (in elements, multiples of 8; both pointers
+ * aligned to 16 bytes), so the query and key heads of a [T, (nq + 2 nkv) d] buffer are one call; y may be x (then ldy =
+ * ldx), otherwise they may not overlap.  Only the columns of the heads are written.  pos: device memory, [n_axes][total_tokens],
+ * any 32-bit values.  The angle is exact to 2e-9 rad at every position.  dtype OB_BF16 or OB_FP32. */
+#define OB_ROTARY_MAX_AXES 8
+#define OB_ROTARY_MAX_HEADS 4096
+typedef struct {
+    int head_dim, n_axes;
+    float base;
+    int per_axis;
+    int8_t axis_of_pair[64];       /* head_dim / 2 of them are read */
+} ob_rotary_axes_desc;
+int ob_rotary_axes(const ob_rotary_axes_desc *desc, const void *x, int ldx, void *y, int ldy, int total_tokens, int n_heads,
+                   const int32_t *pos, int inverse, int dtype, void *hip_stream);
 
 /* T x T byte mask (1 = allowed): allowed(i, j) <=> i and j lie in the same segment (and j <= i when
  * causal), evaluated per entry from cu_seqlens by a small kernel of its own (the attention kernels

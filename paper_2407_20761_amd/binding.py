@@ -60,6 +60,10 @@ class ob_attn_bwd_launch(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("key_rows", "query_rows", "workgroups", "order_rows")]
 
 
+class ob_rotary_axes_desc(C.Structure):
+    _fields_ = [("head_dim", C.c_int), ("n_axes", C.c_int), ("base", C.c_float), ("per_axis", C.c_int), ("axis_of_pair", C.c_int8 * 64)]
+
+
 CONNECTOR_FIELDS = ("n_g", "n_b", "w1", "b1", "w2", "b2")
 
 
@@ -103,6 +107,9 @@ _SIGNATURES = {
     "ob_varlen_attn_bwd_workspace_bytes": (_Z, [_I, _I, _I, _I]),
     "ob_varlen_attn_bwd": (_I, [_P] * 9 + [_I, _I, _I, _SEG, _I, _I, _I, _F, _I, _I, _P, _Z, _P]),
     "ob_varlen_attn_bwd_static": (_I, [_P] * 9 + [_I, _I, _I, _SEG, _I, _I, _I, _F, _I, _I, _P]),
+    "ob_varlen_attn_window_fwd": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _SEG, _I, _I, _I, _F, _I, _I, _I, _P]),
+    "ob_varlen_attn_window_bwd_workspace_bytes": (_Z, [_SEG, _I, _I, _I, _I, _I, _I]),
+    "ob_varlen_attn_window_bwd": (_I, [_P] * 9 + [_I, _I, _I, _SEG, _I, _I, _I, _F, _I, _I, _I, _P, _Z, _P]),
     "ob_block_saved_bytes": (_Z, [_DESC, _I]),
     "ob_block_workspace_bytes": (_Z, [_DESC, _I]),
     "ob_block_saved_offset": (_Z, [_DESC, _I, C.c_char_p]),
@@ -117,6 +124,7 @@ _SIGNATURES = {
     "ob_gemm_act_plan": (_I, [_I, _I, _I, _I, _I, _I, C.POINTER(ob_gemm_launch), C.POINTER(C.c_int)]),
     "ob_varlen_attn_bwd_plan": (_I, [_SEG, _I, _I, _I, _I, C.POINTER(ob_attn_bwd_launch), _i32p, _I]),
     "ob_varlen_attn_bwd_threads": (_I, [_SEG, _I, _I, _I, _I, C.POINTER(C.c_int)]),
+    "ob_rotary_axes": (_I, [C.POINTER(ob_rotary_axes_desc), _P, _I, _P, _I, _I, _I, _P, _I, _I, _P]),
     "ob_debug_materialize_mask": (_I, [_SEG, _I, _P, _P]),
     "ob_connector_saved_bytes": (_Z, [C.POINTER(ob_connector_desc), _I]),
     "ob_connector_workspace_bytes": (_Z, [C.POINTER(ob_connector_desc), _I]),
@@ -239,6 +247,23 @@ def ob_varlen_attn_bwd_static(d_o, q, k, v, o, lse, dq, dk, dv, ldq, ldkv, ldo, 
     _check(lib.ob_varlen_attn_bwd_static(_ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse),
                                          _ptr(dq), _ptr(dk), _ptr(dv), ldq, ldkv, ldo, C.byref(seg.c),
                                          nq, nkv, d, scale, mask, dtype, _stream(stream)))
+
+
+def ob_varlen_attn_window_fwd(q, k, v, o, lse, ldq, ldkv, ldo, seg: Segments, nq, nkv, d, scale, window, sinks=0,
+                              dtype=OB_BF16, stream=None):
+    _check(lib.ob_varlen_attn_window_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), ldq, ldkv, ldo, C.byref(seg.c), nq, nkv, d,
+                                         scale, window, sinks, dtype, _stream(stream)))
+
+
+def ob_varlen_attn_window_bwd_workspace_bytes(seg: Segments, nq, nkv, d, window, sinks=0, dtype=OB_BF16) -> int:
+    return lib.ob_varlen_attn_window_bwd_workspace_bytes(C.byref(seg.c), nq, nkv, d, window, sinks, dtype)
+
+
+def ob_varlen_attn_window_bwd(d_o, q, k, v, o, lse, dq, dk, dv, ldq, ldkv, ldo, seg: Segments, nq, nkv, d, scale, window, sinks,
+                              ws, dtype=OB_BF16, stream=None):
+    _check(lib.ob_varlen_attn_window_bwd(_ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv), ldq,
+                                         ldkv, ldo, C.byref(seg.c), nq, nkv, d, scale, window, sinks, dtype, _ptr(ws), _nbytes(ws),
+                                         _stream(stream)))
 
 
 def ob_block_saved_bytes(desc, total_tokens) -> int:
@@ -366,6 +391,19 @@ def ob_connector_bwd(desc, weights: dict, grads: dict, flags, v, dx_llm, dv, n_t
     _check(lib.ob_connector_bwd(C.byref(desc), C.byref(w), C.byref(g), int(flags), _ptr(v), _ptr(dx_llm),
                                 _ptr(dv), n_tiles, dst_rows.host_ptr, _ptr(dst_rows.dev), llm_tokens,
                                 _ptr(saved), _nbytes(saved), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def make_rotary_axes_desc(axis_of_pair, head_dim, base=10000.0, per_axis=False) -> ob_rotary_axes_desc:
+    """axis_of_pair: the axis of each of the head_dim / 2 pairs, -1 for a pair that passes"""
+    axes = [int(a) for a in axis_of_pair]
+    if len(axes) != head_dim // 2 or not 1 <= len(axes) <= 64:
+        raise ValueError(f"{len(axes)} pairs given, a head of {head_dim} has {head_dim // 2} (at most 64)")
+    return ob_rotary_axes_desc(int(head_dim), max(0, *axes) + 1, float(base), int(bool(per_axis)), (C.c_int8 * 64)(*axes))
+
+
+def ob_rotary_axes(desc, x, ldx, y, ldy, total_tokens, n_heads, pos, inverse=False, dtype=OB_BF16, stream=None):
+    _check(lib.ob_rotary_axes(C.byref(desc), _ptr(x), ldx, _ptr(y), ldy, total_tokens, n_heads, _ptr(pos), int(bool(inverse)), dtype,
+                              _stream(stream)))
 
 
 def ob_debug_materialize_mask(seg: Segments, mask, out, stream=None):

@@ -57,7 +57,6 @@ ProfScope::~ProfScope() {
 
 namespace {
 
-constexpr int MAX_TOKENS = 1 << 22;
 constexpr int MAX_HIDDEN = 8192;  // row-wise kernels keep one row in registers
 
 int validate_segments(const ob_segments *seg, const char *who) {

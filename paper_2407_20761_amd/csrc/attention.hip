@@ -276,8 +276,10 @@ __device__ __forceinline__ int head_of_slot(int hs, int heads) {
 // workgroup gives each segment's first tile number, and the thread whose range holds `tile`
 // publishes the answer -- one global-memory round trip instead of a serial walk over cu.
 struct TileInfo { int seg_start, seg_end, row0; };
+// LONGER: segments of at most `longer_than` rows have no tiles.
+template <bool LONGER = false>
 __device__ __forceinline__ TileInfo find_tile(const int32_t *__restrict__ cu, int n_seg, int tile_rows,
-                                              int *sh /* >= 8 ints */, int tile) {
+                                              int *sh /* >= 8 ints */, int tile, int longer_than = 0) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool scans = tid < 256;  // waves past the fourth only take part in the barriers
     if (tid == 0) sh[2] = -1;
@@ -288,7 +290,7 @@ __device__ __forceinline__ TileInfo find_tile(const int32_t *__restrict__ cu, in
         if (scans && j < n_seg) {
             a = cu[j];
             b = cu[j + 1];
-            nt = (b - a + tile_rows - 1) / tile_rows;
+            nt = !LONGER || b - a > longer_than ? (b - a + tile_rows - 1) / tile_rows : 0;
         }
         int incl = nt;  // inclusive scan inside the wave
 #pragma unroll
@@ -333,9 +335,50 @@ __device__ __forceinline__ TileInfo pick_tile(const TileOrder &ord, int rank, co
     return t;
 }
 
+// What a causal row sees of the keys in front of it: all of its segment, or with a window the last `window` keys (its own
+// among them) and the segment's first `sinks`.  Of dK / dV the two parts of a windowed launch differ: Band owns tiles of key rows and
+// walks the queries whose window reaches them, Sinks owns the first keys of a segment longer than the window, which every row sees, and a
+// chunk of the segment's queries (see launch_attn_window_bwd()).
+// A windowed launch loads nothing of another segment (rows past the end of its own arrive as zeros): no value there, infinite or
+// not a number, can reach it.
+struct Whole { static constexpr bool BAND = false, SINKS = false; };
+struct Band { static constexpr bool BAND = true, SINKS = false; int window, sinks; };
+struct Sinks { static constexpr bool BAND = false, SINKS = true; int window, sinks, chunk; float *part; };
+
 // ------------------------------------------------------------------------------------------------
 // forward:  S^T = K Q^T,  online softmax per lane,  O^T += V^T P^T
 // ------------------------------------------------------------------------------------------------
+// The key tiles that a workgroup of 128 query rows walks.  With a window: the segment's first tile for the sinks, where the band does not start
+// in it, then those of the band; n_head tiles from the start need a mask, as some row's window begins in or behind them, and `skip` tiles
+// of the segment in front of the band are left out.
+template <class WIN>
+struct BandTiles {
+    static constexpr int skip = 0, n_head = 0, sink_end = 0;
+    __device__ __forceinline__ BandTiles(const TileInfo &, const WIN &, int) {}
+    __device__ __forceinline__ int row(int j) const { return j * ST; }       // first key row of tile j, from the segment's start
+    __device__ __forceinline__ int from(int) const { return 0; }             // first key of a row's band
+    __device__ __forceinline__ bool wave_sees(int, int) const { return true; }
+};
+template <>
+struct BandTiles<Band> {
+    int window, skip, n_head, sink_end, wave_from;
+    bool apart;          // the sinks have a tile of their own
+    __device__ __forceinline__ BandTiles(const TileInfo &ti, const Band &win, int wave) {
+        window = win.window;
+        sink_end = min(ti.seg_start + win.sinks, ti.seg_end);
+        wave_from = ti.row0 + wave * 32 - window + 1;
+        const int len_front = ti.row0 - ti.seg_start, last = min(ti.row0 + QT, ti.seg_end) - 1 - ti.seg_start;
+        const int first = max(0, len_front - window + 1) / ST;               // first tile of the band
+        const int whole = max(0, last - window + 1 + ST - 1) / ST;           // first that lies in every row's window
+        apart = first > 0 && win.sinks > 0;
+        skip = apart ? first - 1 : first;
+        n_head = min(whole, (last + ST) / ST) - skip;
+    }
+    __device__ __forceinline__ int row(int j) const { return (apart && j == 0 ? 0 : j + skip) * ST; }
+    __device__ __forceinline__ int from(int q_row) const { return q_row - window + 1; }
+    __device__ __forceinline__ bool wave_sees(int kv_first, int rows) const { return kv_first + rows > wave_from || kv_first < sink_end; }
+};
+
 // LDS reads are issued one batch ahead of the MFMAs that consume them (explicit double buffers and
 // scheduling groups): left alone, the compiler emits read / wait / MFMA triples and every MFMA
 // pays a full LDS round trip.
@@ -346,11 +389,12 @@ __device__ __forceinline__ TileInfo pick_tile(const TileOrder &ord, int rank, co
         __builtin_amdgcn_sched_barrier(0);                         \
     } while (0)
 
-template <int D, bool CAUSAL, bool MASK>
+// BAND: keys in front of `from` are seen below `sink_end` alone.
+template <int D, bool CAUSAL, bool MASK, bool BAND = false>
 __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict__ ks,
                                          const unsigned char OB_LDS *__restrict__ vs, const Tile<D> &tl,
                                          const bf16x8 (&qf)[D / 16], f32x16 (&acc_o)[D / 32], float &m_run,
-                                         float &l_run, int kv0, int seg_end, int q_row, float sl2) {
+                                         float &l_run, int kv0, int seg_end, int q_row, float sl2, int from = 0, int sink_end = 0) {
     const int lh = (threadIdx.x & 63) >> 5;
     constexpr int HB = 2;                 // K fragments (D-steps) per batch
     constexpr int R = D == 128 ? 3 : 2;   // batches in flight (ring depth)
@@ -393,7 +437,7 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int kv = kv0 + mt * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
-                const bool ok = kv < seg_end && (!CAUSAL || kv <= q_row);
+                const bool ok = kv < seg_end && (!CAUSAL || kv <= q_row) && (!BAND || kv >= from || kv < sink_end);
                 const float s = ok ? acc_s[mt][r] : NEG_BIG;
                 acc_s[mt][r] = s;
                 mx = fmaxf(mx, s);
@@ -420,7 +464,8 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
             for (int r = 0; r < 16; ++r) acc_o[i][r] *= alpha;
         m_run = m_new;
     }
-    const float c = m_run * sl2;
+    // (a row may see nothing of the first tiles of its band: its maximum is then that of masked scores, whose exponentials have to be 0)
+    const float c = (BAND && MASK ? fmaxf(m_run, 0.5f * NEG_BIG) : m_run) * sl2;
     float psum = 0.f;
     // The exponentials of contraction step u + 1 (8 per lane, then their rounding to bf16) are issued
     // between the MFMAs of step u, one MFMA to a few vector instructions: a wave's own element-wise
@@ -465,11 +510,11 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
 }
 
 // (D = 64: 128 registers, four waves on a SIMD)
-template <int D, bool CAUSAL>
+template <int D, bool CAUSAL, class WIN = Whole>
 __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
     const __bf16 *__restrict__ q, const __bf16 *__restrict__ k, const __bf16 *__restrict__ v,
     __bf16 *__restrict__ o, float *__restrict__ lse, int ldq, int ldkv, int ldo,
-    const int32_t *__restrict__ cu, int n_seg, int T, int group, float scale, int heads, TileOrder ord) {
+    const int32_t *__restrict__ cu, int n_seg, int T, int group, float scale, int heads, TileOrder ord, WIN win) {
     __shared__ __attribute__((aligned(1024))) unsigned char k_s0[Tile<D>::BYTES];
     __shared__ __attribute__((aligned(1024))) unsigned char v_s0[Tile<D>::BYTES];
     __shared__ __attribute__((aligned(1024))) unsigned char k_s1[Tile<D>::BYTES];
@@ -490,7 +535,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
     tl.init(ldkv, wave, lane);
     const unsigned char *kbase = (const unsigned char *)(k + kvh * D);
     const unsigned char *vbase = (const unsigned char *)(v + kvh * D);
-    const long kv_bytes = (long)T * ldkv * 2 - (long)kvh * D * 2;  // from kbase / vbase to the end
+    const long kv_bytes = (long)(WIN::BAND ? ti.seg_end : T) * ldkv * 2 - (long)kvh * D * 2;  // from kbase / vbase to the end
 
     bf16x8 qf[D / 16];
 #pragma unroll
@@ -503,37 +548,43 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
         for (int r = 0; r < 16; ++r) acc_o[i][r] = 0.f;
     float m_run = NEG_BIG, l_run = 0.f;
 
+    const BandTiles<WIN> bt(ti, win, wave);
     const int kv_end = CAUSAL ? min(ti.seg_end, ti.row0 + QT) : ti.seg_end;
-    const int n_tiles = (kv_end - ti.seg_start + ST - 1) / ST;
+    const int n_tiles = (kv_end - ti.seg_start + ST - 1) / ST - bt.skip;
     unsigned char OB_LDS *const ks0 = (unsigned char OB_LDS *)k_s0, *const ks1 = (unsigned char OB_LDS *)k_s1;
     unsigned char OB_LDS *const vs0 = (unsigned char OB_LDS *)v_s0, *const vs1 = (unsigned char OB_LDS *)v_s1;
     {
-        const long off = (long)ti.seg_start * ldkv * 2;
+        const long off = (long)(ti.seg_start + bt.row(0)) * ldkv * 2;
         tl.issue(kbase + off, kv_bytes - off, ks0, wave);
         tl.issue(vbase + off, kv_bytes - off, vs0, wave);
     }
     // Tiles before the workgroup's first row (causal) or before the ragged end need no mask; they
     // run in a loop of their own whose body is a single straight path (with several paths per
     // iteration the register allocator shuffles the accumulators between homes every iteration).
-    const int n_main = CAUSAL ? (ti.row0 - ti.seg_start) / ST : (ti.seg_end - ti.seg_start) / ST;
+    const int n_main = (CAUSAL ? (ti.row0 - ti.seg_start) / ST : (ti.seg_end - ti.seg_start) / ST) - bt.skip;
     int j = 0;
 #define OB_FWD_ITER(MASKED, KS, VS, KS_NEXT, VS_NEXT)                                                     \
     {                                                                                                    \
-        const int kv0 = ti.seg_start + j * ST;                                                           \
+        const int kv0 = ti.seg_start + bt.row(j);                                                          \
         __builtin_amdgcn_s_waitcnt(WAIT_VM0);                                                            \
         __syncthreads();                                                                                 \
         if (j + 1 < n_tiles) {                                                                           \
-            const long off = (long)(kv0 + ST) * ldkv * 2;                                                \
+            const long off = (long)(WIN::BAND ? ti.seg_start + bt.row(j + 1) : kv0 + ST) * ldkv * 2;                                                \
             tl.issue(kbase + off, kv_bytes - off, (KS_NEXT), wave);                                      \
             tl.issue(vbase + off, kv_bytes - off, (VS_NEXT), wave);                                      \
         }                                                                                                \
         if (!(MASKED))                                                                                   \
             fwd_tile<D, CAUSAL, false>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0, ti.seg_end, q_row,  \
                                        sl2);                                                             \
-        else if (!(CAUSAL && kv0 > wave_q_last))                                                         \
-            fwd_tile<D, CAUSAL, true>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0, ti.seg_end, q_row,   \
-                                      sl2);                                                              \
+        else if (!(CAUSAL && kv0 > wave_q_last) && bt.wave_sees(kv0, ST))                                \
+            fwd_tile<D, CAUSAL, true, WIN::BAND>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0,           \
+                                                 ti.seg_end, q_row, sl2, bt.from(q_row), bt.sink_end);   \
         ++j;                                                                                             \
+    }
+#define OB_FWD_ANY(MASKED) OB_FWD_ITER(MASKED, (j & 1) ? ks1 : ks0, (j & 1) ? vs1 : vs0, (j & 1) ? ks0 : ks1, (j & 1) ? vs0 : vs1)
+    if constexpr (WIN::BAND) {
+        while (j < bt.n_head) OB_FWD_ANY(true)
+        if ((j & 1) && j < n_main) OB_FWD_ANY(false)
     }
     // two tiles per trip: the stage buffers are then compile-time constants and every LDS address is
     // a register plus an immediate offset
@@ -541,7 +592,6 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
         OB_FWD_ITER(false, ks0, vs0, ks1, vs1)
         OB_FWD_ITER(false, ks1, vs1, ks0, vs0)
     }
-#define OB_FWD_ANY(MASKED) OB_FWD_ITER(MASKED, (j & 1) ? ks1 : ks0, (j & 1) ? vs1 : vs0, (j & 1) ? ks0 : ks1, (j & 1) ? vs0 : vs1)
     while (j < n_main) OB_FWD_ANY(false)
     while (j < n_tiles) OB_FWD_ANY(true)
 #undef OB_FWD_ANY
@@ -574,12 +624,12 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
 // on one half of the tile with their partial dQ added at the end, asked the L2 for twice the bytes
 // per MFMA (4.7 GB per launch on the 7B-shaped batch, 10 TB/s) and had a barrier per 24 MFMAs.
 // ------------------------------------------------------------------------------------------------
-template <int D, bool CAUSAL, bool MASK>
+template <int D, bool CAUSAL, bool MASK, bool BAND = false>
 __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__ ks,
                                         const unsigned char OB_LDS *__restrict__ vs, const Tile<D> &tl,
                                         const bf16x8 (&qf)[D / 16], const bf16x8 (&dof)[D / 16],
                                         f32x16 (&acc_dq)[D / 32], float lse2, float dlt, int kv_first,
-                                        int seg_end, int q_row, float sl2) {
+                                        int seg_end, int q_row, float sl2, int from = 0, int sink_end = 0) {
     // ks / vs point at a 32-row half of the K / V tile; kv_first is its first key row
     const int lh = (threadIdx.x & 63) >> 5;
     constexpr int HB = 2;             // D-steps per batch (a batch reads HB fragments of K and HB of V)
@@ -624,7 +674,7 @@ __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__
             bool ok = true;
             if (MASK) {
                 const int kv = kv_first + 8 * (r >> 2) + 4 * lh + (r & 3);
-                ok = kv < seg_end && (!CAUSAL || kv <= q_row);
+                ok = kv < seg_end && (!CAUSAL || kv <= q_row) && (!BAND || kv >= from || kv < sink_end);
             }
             const float p = ok ? fast_exp2(acc_s[r] * sl2 - lse2) : 0.f;
             o[e] = (__bf16)(p * (acc_dp[r] - dlt));
@@ -652,13 +702,13 @@ __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__
     OB_SCHED_READS_THEN_MFMA(0, DT);
 }
 
-template <int D, bool CAUSAL>
+template <int D, bool CAUSAL, class WIN = Whole>
 __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
     const __bf16 *__restrict__ d_o, const __bf16 *__restrict__ q, const __bf16 *__restrict__ k,
     const __bf16 *__restrict__ v, const __bf16 *__restrict__ o, const float *__restrict__ lse,
     float *__restrict__ lse2_all, float *__restrict__ delta, __bf16 *__restrict__ dq, int ldq, int ldkv, int ldo,
     const int32_t *__restrict__ cu, int n_seg, int T, int group, float scale, float rot_log2_base, int heads,
-    TileOrder ord) {
+    TileOrder ord, WIN win) {
     __shared__ __attribute__((aligned(1024))) unsigned char k_s0[Tile<D>::BYTES];
     __shared__ __attribute__((aligned(1024))) unsigned char v_s0[Tile<D>::BYTES];
     __shared__ __attribute__((aligned(1024))) unsigned char k_s1[Tile<D>::BYTES];
@@ -681,7 +731,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
     tl.init(ldkv, wave, lane);
     const unsigned char *kbase = (const unsigned char *)(k + kvh * D);
     const unsigned char *vbase = (const unsigned char *)(v + kvh * D);
-    const long kv_bytes = (long)T * ldkv * 2 - (long)kvh * D * 2;
+    const long kv_bytes = (long)(WIN::BAND ? ti.seg_end : T) * ldkv * 2 - (long)kvh * D * 2;
 
     bf16x8 qf[D / 16], dof[D / 16];
 #pragma unroll
@@ -711,24 +761,25 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc_dq[i][r] = 0.f;
 
+    const BandTiles<WIN> bt(ti, win, wave);
     const int kv_end = CAUSAL ? min(ti.seg_end, ti.row0 + QT) : ti.seg_end;
-    const int n_tiles = (kv_end - ti.seg_start + ST - 1) / ST;
+    const int n_tiles = (kv_end - ti.seg_start + ST - 1) / ST - bt.skip;
     unsigned char OB_LDS *const ks0 = (unsigned char OB_LDS *)k_s0, *const ks1 = (unsigned char OB_LDS *)k_s1;
     unsigned char OB_LDS *const vs0 = (unsigned char OB_LDS *)v_s0, *const vs1 = (unsigned char OB_LDS *)v_s1;
     {
-        const long off = (long)ti.seg_start * ldkv * 2;
+        const long off = (long)(ti.seg_start + bt.row(0)) * ldkv * 2;
         tl.issue(kbase + off, kv_bytes - off, ks0, wave);
         tl.issue(vbase + off, kv_bytes - off, vs0, wave);
     }
-    const int n_main = CAUSAL ? (ti.row0 - ti.seg_start) / ST : (ti.seg_end - ti.seg_start) / ST;
+    const int n_main = (CAUSAL ? (ti.row0 - ti.seg_start) / ST : (ti.seg_end - ti.seg_start) / ST) - bt.skip;
     int j = 0;
 #define OB_DQ_ITER(MASKED, KS, VS, KS_NEXT, VS_NEXT)                                                          \
     {                                                                                                        \
-        const int kv0 = ti.seg_start + j * ST;                                                               \
+        const int kv0 = ti.seg_start + bt.row(j);                                                              \
         __builtin_amdgcn_s_waitcnt(WAIT_VM0);                                                                \
         __syncthreads();                                                                                     \
         if (j + 1 < n_tiles) {                                                                               \
-            const long off = (long)(kv0 + ST) * ldkv * 2;                                                    \
+            const long off = (long)(WIN::BAND ? ti.seg_start + bt.row(j + 1) : kv0 + ST) * ldkv * 2;                                                    \
             tl.issue(kbase + off, kv_bytes - off, (KS_NEXT), wave);                                          \
             tl.issue(vbase + off, kv_bytes - off, (VS_NEXT), wave);                                          \
         }                                                                                                    \
@@ -738,17 +789,23 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
                 if (wave_live)                                                                               \
                     dq_half<D, CAUSAL, false>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, acc_dq, lse2,  \
                                               dlt, kv_first, ti.seg_end, q_row, sl2);                        \
-            } else if (wave_live && kv_first < ti.seg_end && !(CAUSAL && kv_first > wave_q_last))            \
-                dq_half<D, CAUSAL, true>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, acc_dq, lse2, dlt,  \
-                                         kv_first, ti.seg_end, q_row, sl2);                                  \
+            } else if (wave_live && kv_first < ti.seg_end && !(CAUSAL && kv_first > wave_q_last) &&          \
+                       bt.wave_sees(kv_first, 32))                                                           \
+                dq_half<D, CAUSAL, true, WIN::BAND>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, acc_dq,  \
+                                                    lse2, dlt, kv_first, ti.seg_end, q_row, sl2,             \
+                                                    bt.from(q_row), bt.sink_end);                            \
         }                                                                                                    \
         ++j;                                                                                                 \
+    }
+#define OB_DQ_ANY(MASKED) OB_DQ_ITER(MASKED, (j & 1) ? ks1 : ks0, (j & 1) ? vs1 : vs0, (j & 1) ? ks0 : ks1, (j & 1) ? vs0 : vs1)
+    if constexpr (WIN::BAND) {
+        while (j < bt.n_head) OB_DQ_ANY(true)
+        if ((j & 1) && j < n_main) OB_DQ_ANY(false)
     }
     while (j + 1 < n_main) {  // two tiles per trip: the stage buffers are compile-time constants
         OB_DQ_ITER(false, ks0, vs0, ks1, vs1)
         OB_DQ_ITER(false, ks1, vs1, ks0, vs0)
     }
-#define OB_DQ_ANY(MASKED) OB_DQ_ITER(MASKED, (j & 1) ? ks1 : ks0, (j & 1) ? vs1 : vs0, (j & 1) ? ks0 : ks1, (j & 1) ? vs0 : vs1)
     while (j < n_main) OB_DQ_ANY(false)
     while (j < n_tiles) OB_DQ_ANY(true)
 #undef OB_DQ_ANY
@@ -812,9 +869,10 @@ __device__ __forceinline__ void dkv_scores(const unsigned char OB_LDS *__restric
 
 // role P: probabilities of the 32 MT x 32 score tile, packed as the second operands of the 2 MT
 // 16-row contraction steps (pk[mt][h] serves step 2 mt + h)
-template <bool CAUSAL, bool MASK, int MT>
+// (BAND: rows `window` and more behind the key do not see it)
+template <bool CAUSAL, bool MASK, int MT, bool BAND = false>
 __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned char OB_LDS *__restrict__ lse2_s,
-                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2]) {
+                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2], int window = 0) {
     const int lh = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -827,7 +885,7 @@ __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned 
                 bool ok = true;
                 if (MASK) {
                     const int qr = q0 + mt * 32 + 8 * g + 4 * lh + e;
-                    ok = qr < seg_end && (!CAUSAL || kv_row <= qr);
+                    ok = qr < seg_end && (!CAUSAL || kv_row <= qr) && (!BAND || qr - kv_row < window);
                 }
                 const float pe = fast_exp2(s[mt][4 * g + e] * sl2 - l4[e]);
                 p[4 * g + e] = ok ? pe : 0.f;
@@ -1011,6 +1069,16 @@ struct DkvWalk {
         n_masked = group * (n_diag + n_end);
         n_all = n_masked + group * n_mid;
     }
+    // Rows [q_begin, q_end), `head` masked tiles in front, the first `free_rows` rows otherwise without a mask
+    __device__ __forceinline__ DkvWalk(int q_begin_, int q_end, int head, int free_rows, int group) : q_begin(q_begin_), dead(0) {
+        const int n_iter = (q_end - q_begin + SR - 1) / SR;
+        n_head = n_diag = min(head, n_iter);
+        const int n_mid_end = max(n_head, free_rows / SR);
+        n_end = n_iter - n_mid_end;
+        n_mid = n_mid_end - n_head;
+        n_masked = group * (n_diag + n_end);
+        n_all = n_masked + group * n_mid;
+    }
     // first query row of masked tile j of a head
     __device__ __forceinline__ int masked_row(int j) const {
         const int diag = dead + j, end = n_head + n_mid + j - n_diag;
@@ -1030,13 +1098,14 @@ struct DkvRequests {
     const unsigned char *base;
     const float *stat_base;
     long ld2;                     // bytes from row to row
-    int T, head0, group, piece0;  // the wave's first piece
+    int T, rows_end;              // rows of a head's statistics, rows that there are
+    int head0, group, piece0;     // the wave's first piece
     uint32_t (&first)[LD], voff[LD], stat_voff;
     int n_issued, run_left, part_left, part_row, part_head, next_part, next_head;
     u32x4 rsrc, stat_rsrc;
-    __device__ __forceinline__ DkvRequests(const DkvWalk<D, CAUSAL, KVT, SR> &walk, const void *base_, long ld2_, const float *stat_, int T_,
+    __device__ __forceinline__ DkvRequests(const DkvWalk<D, CAUSAL, KVT, SR> &walk, const void *base_, long ld2_, const float *stat_, int T_, int rows_end_,
                                            int head0_, int group_, int piece0_, uint32_t (&first_)[LD])
-        : w(walk), base((const unsigned char *)base_), stat_base(stat_), ld2(ld2_), T(T_), head0(head0_), group(group_), piece0(piece0_), first(first_),
+        : w(walk), base((const unsigned char *)base_), stat_base(stat_), ld2(ld2_), T(T_), rows_end(rows_end_), head0(head0_), group(group_), piece0(piece0_), first(first_),
           stat_voff(0), n_issued(0), run_left(0), part_left(0), part_row(0), part_head(0),
           next_part(walk.n_masked == 0 ? 2 : walk.n_diag > 0 ? 0 : 1), next_head(0),
           rsrc{0, 0, 0, 0}, stat_rsrc{0, 0, 0, 0} {}
@@ -1053,8 +1122,8 @@ struct DkvRequests {
         }
         run_left = APART ? 1 : min(part_left, dkv_run((uint32_t)ld2, SR));
         const long off = (long)part_row * ld2 + (long)part_head * D * 2;
-        rsrc = make_rsrc(base + off, (long)T * ld2 - off);
-        stat_rsrc = make_rsrc(stat_base + (size_t)part_head * T + part_row, (long)(T - part_row) * 4);
+        rsrc = make_rsrc(base + off, (long)rows_end * ld2 - off);
+        stat_rsrc = make_rsrc(stat_base + (size_t)part_head * T + part_row, (long)(rows_end - part_row) * 4);
 #pragma unroll
         for (int p = 0; p < LD; ++p) voff[p] = first[p];
         stat_voff = lane * 4;
@@ -1067,7 +1136,7 @@ struct DkvRequests {
         const int in_tile = (piece0 + (P < SKIP ? P : P + SKIP)) * Tile<D, SR>::RPI;      // the piece's first row
         const long off = (long)(part_row - SR + in_tile) * ld2 + (long)part_head * D * 2;
         voff[P] = dkv_piece_offset(first[P], in_tile, (uint32_t)ld2);
-        load_lds16<1, SKIP, P>(make_rsrc(base + off, (long)T * ld2 - off), pieces, voff);
+        load_lds16<1, SKIP, P>(make_rsrc(base + off, (long)rows_end * ld2 - off), pieces, voff);
         if constexpr (P + 1 < LD) issue_apart<P + 1>(pieces);
     }
     // the next tile: the wave's pieces of it to `pieces`, if `copies`; its statistics to stat, if `stats`
@@ -1088,13 +1157,13 @@ struct DkvRequests {
     }
 };
 
-template <int D, bool CAUSAL, int NP, int SR, bool APART = false>
+template <int D, bool CAUSAL, int NP, int SR, bool APART = false, class WIN = Whole>
 __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 2) void attn_bwd_dkv_kernel(
     const __bf16 *__restrict__ d_o, const __bf16 *__restrict__ q, const __bf16 *__restrict__ k,
     const __bf16 *__restrict__ v, const float *__restrict__ lse2_all, const float *__restrict__ delta,
     __bf16 *__restrict__ dk, __bf16 *__restrict__ dv, int ldq, int ldkv, int ldo,
     const int32_t *__restrict__ cu, int n_seg, int T, int group, float scale, float rot_log2_base, int heads,
-    TileOrder ord) {
+    TileOrder ord, WIN win) {
     // three stages of the streamed Q and dO tiles (the results are formed one tile behind the scores, see
     // below), two buffers for the probabilities on their way from one role to the other, row statistics
     __shared__ __attribute__((aligned(1024))) unsigned char tiles_s[6 * Tile<D, SR>::BYTES];
@@ -1103,8 +1172,22 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
     __shared__ __attribute__((aligned(256))) unsigned char stat_s[6 * 256];    // lse2 x 3 stages, Delta x 3 stages
     __shared__ int sh[8];
     const int rank = blockIdx.x / heads;
-    const TileInfo ti = pick_tile<true>(ord, rank, cu, n_seg, KVT, sh);
-    if (ti.row0 < 0) return;
+    TileInfo ti;
+    int q_chunk = 0, window = 0;      // (Sinks) first of the workgroup's query rows; (Band) the window
+    if constexpr (WIN::SINKS) {
+        ti = find_tile<true>(cu, n_seg, win.chunk, sh, rank, win.window);
+        q_chunk = ti.row0;
+        ti.row0 = ti.seg_start;
+    } else {
+        ti = pick_tile<true>(ord, rank, cu, n_seg, KVT, sh);
+        if (ti.row0 < 0) return;
+    }
+    int q_end = ti.seg_end, rows_end = T;
+    if constexpr (WIN::BAND) {
+        window = win.window;
+        rows_end = q_end = min(ti.seg_end, ti.row0 + KVT - 1 + window);
+    }
+    if constexpr (WIN::SINKS) rows_end = q_end = min(ti.seg_end, q_chunk + win.chunk);
     // one workgroup per key/value head: the group's query heads run one after another
     const int kvh = head_of_slot(blockIdx.x - rank * heads, heads);
     const int lane = threadIdx.x & 63, lx = lane & 31, lh = lane >> 5;
@@ -1114,6 +1197,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
     const int kv_row = min(ti.row0 + pair * 32 + lx, ti.seg_end - 1);
     const bool kv_live = ti.row0 + pair * 32 + lx < ti.seg_end;
     const int pair_kv_first = ti.row0 + pair * 32;
+    auto band_is_past = [&](int q0) __attribute__((always_inline)) { return q0 - (pair_kv_first + 31) >= window; };
     const float sl2 = scale * LOG2E;
     constexpr int KT = D / 16, DT = D / 32;
     constexpr bool FUSE = NP == 2 && SR == 64;      // one or two waves to a SIMD: element-wise work between the wave's own products
@@ -1129,7 +1213,14 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
 
     constexpr int BYTES = Tile<D, SR>::BYTES;
 
-    const DkvWalk<D, CAUSAL, KVT, SR> w(ti, group);
+    const auto w = [&] {
+        if constexpr (WIN::BAND)
+            return DkvWalk<D, CAUSAL, KVT, SR>(ti.row0, q_end, KVT / SR, min(ti.seg_end - ti.row0, win.window), group);
+        else if constexpr (WIN::SINKS)
+            return DkvWalk<D, CAUSAL, KVT, SR>(q_chunk, q_end, q_chunk == ti.seg_start ? KVT / SR : 0, q_end - q_chunk, group);
+        else
+            return DkvWalk<D, CAUSAL, KVT, SR>(ti, group);
+    }();
 
     // the whole walk once per role, chosen outside the loops: each role's loop then carries only its own registers
     auto walk = [&](auto role_tag) __attribute__((always_inline)) {
@@ -1151,7 +1242,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
 #pragma unroll
     for (int p = 0; p < LDW; ++p) first[p] = tl.voff[p % TLD] + (p < TLD ? 0u : (uint32_t)(SR / 2 * ld2));
     unsigned char OB_LDS *const pieces = tiles + OWN_AT + pair * TLD * 1024;
-    DkvRequests<D, CAUSAL, KVT, SR, LDW, TLD, APART> req(w, RG ? d_o : q, ld2, RG ? delta : lse2_all, T, kvh * group, group, pair * TLD, first);
+    DkvRequests<D, CAUSAL, KVT, SR, LDW, TLD, APART> req(w, RG ? d_o : q, ld2, RG ? delta : lse2_all, T, rows_end, kvh * group, group, pair * TLD, first);
     auto request = [&](int stage) __attribute__((always_inline)) {
         req.issue(pieces + stage * BYTES, pair < 4, stat + stage * 256, pair == 0, lane);
     };
@@ -1183,7 +1274,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
         bare_barrier();
         if (GEN) request(NEXT);      // (the masked tiles' trips are short and each takes a descriptor of its own)
         // (GEN: one after the other, each step behind a test)  a masked tile entirely before this pair's keys contributes nothing
-        const bool live = !GEN || (n < w.n_all && !(MASK && CAUSAL && q0 + SR - 1 < pair_kv_first));
+        const bool live = !GEN || (n < w.n_all && !(MASK && CAUSAL && q0 + SR - 1 < pair_kv_first) && !(WIN::BAND && MASK && band_is_past(q0)));
         unsigned char OB_LDS *const p_new = p_mine + (n & 1) * (NP * PB), *const p_old = p_mine + ((n & 1) ^ 1) * (NP * PB);
         const bool late = !GEN || (RG ? live_prev : owed);
         if constexpr (!RG) {
@@ -1197,7 +1288,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
                 for (int i = 0; i < 2 * MT; ++i) pk[i >> 1][i & 1] = pn[i >> 1][i & 1];
             } else {
                 if (FUSE && late) dkv_outputs<D, MT>(tiles + PREV * BYTES, tl, pk, acc_out);
-                if (live) dkv_probs<CAUSAL, MASK, MT>(acc_x, stat + S * 256, q0, ti.seg_end, kv_row, sl2, pk);
+                if (live) dkv_probs<CAUSAL, MASK, MT, WIN::BAND>(acc_x, stat + S * 256, q0, q_end, kv_row, sl2, pk, window);
             }
             if (live) {
 #pragma unroll
@@ -1256,6 +1347,22 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
     while (n <= w.n_all) slow(std::false_type{}, false);
     };
     if (role_g) walk(std::true_type{}); else walk(std::false_type{});
+    if constexpr (WIN::SINKS) {
+        // fp32 sums of the chunk: [slot][key/value head][dV, dK][sink][D]
+        const int sink = pair * 32 + lx;
+        if (!kv_live || sink >= win.sinks) return;
+        float *const dst = win.part + ((((size_t)rank * heads + kvh) * 2 + (role_g ? 1 : 0)) * win.sinks + sink) * D;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(f32x4 *)(dst + dt * 32 + g * 8 + lh * 4) = f32x4{acc_out[dt][4 * g], acc_out[dt][4 * g + 1], acc_out[dt][4 * g + 2], acc_out[dt][4 * g + 3]};
+        return;
+    }
+    // (the sinks of a segment longer than the window come from the sums over its chunks)
+    if constexpr (WIN::BAND) {
+        if (kv_row - ti.seg_start < win.sinks && ti.seg_end - ti.seg_start > win.window) return;
+    }
     if (!kv_live) return;
     // dV^T / dK^T of the whole group of query heads sit in the accumulators: one rounding to bf16
     const float out_scale = role_g ? scale : 1.0f;
@@ -1299,7 +1406,7 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
     const __bf16 *__restrict__ v, const float *__restrict__ lse2_all, const float *__restrict__ delta,
     __bf16 *__restrict__ dk, __bf16 *__restrict__ dv, int ldq, int ldkv, int ldo,
     const int32_t *__restrict__ cu, int n_seg, int T, int group, float scale, float rot_log2_base, int heads,
-    TileOrder ord) {
+    TileOrder ord, Whole) {
     using B = DkvBlocks;
     constexpr int D = B::D, SR = B::SR, KT = D / 16, BUF = B::BUF, LD = Tile<D, SR>::LD;
     __shared__ __attribute__((aligned(1024))) unsigned char lds_s[B::TOTAL];
@@ -1343,7 +1450,7 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
     unsigned char OB_LDS *const p_blk = lds + B::P_AT + (b * 2 + a) * B::BLK + lane * 16;       // own block of the scores
     unsigned char OB_LDS *const ds_blk = lds + B::DS_AT + (b * 2 + a) * B::BLK + lane * 16;
     unsigned char OB_LDS *const out_blk = lds + (RG ? B::DS_AT : B::P_AT) + b * 2 * B::BLK + lane * 16;   // the four steps of a result
-    DkvRequests<D, CAUSAL, B::KVT, SR, LD> req(w, RG ? d_o : q, (RG ? (long)ldo : (long)ldq) * 2, RG ? delta : lse2_all, T, kvh * group, group,
+    DkvRequests<D, CAUSAL, B::KVT, SR, LD> req(w, RG ? d_o : q, (RG ? (long)ldo : (long)ldq) * 2, RG ? delta : lse2_all, T, T, kvh * group, group,
                                               w4 * LD, tl.voff);
     auto next = [](int stage, int stages) __attribute__((always_inline)) { return stage + 1 == stages ? 0 : stage + 1; };
     int st_issue = 0, st_stat_issue = 0;                                       // stages of the tile to request next
@@ -1482,6 +1589,41 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
         }
 }
 
+// dK and dV of the sinks of every segment longer than the window: the fp32 sums of its chunks, in order, then one rounding.  Workgroups
+// (place, key/value head, 1024 elements), those of a segment's first chunk at work.
+template <int D>
+__global__ __launch_bounds__(256) void attn_sink_sum_kernel(const float *__restrict__ part, __bf16 *__restrict__ dk, __bf16 *__restrict__ dv,
+                                                            int ldkv, const int32_t *__restrict__ cu, int n_seg, Sinks win, float scale) {
+    __shared__ int sh[8];
+    const int place = blockIdx.x, kvh = blockIdx.y, nkv = gridDim.y;
+    const TileInfo ti = find_tile<true>(cu, n_seg, win.chunk, sh, place, win.window);
+    if (ti.row0 != ti.seg_start) return;
+    const int len = ti.seg_end - ti.seg_start, chunks = (len + win.chunk - 1) / win.chunk;
+    const int e = (blockIdx.z * 256 + threadIdx.x) * 4, role = e / (win.sinks * D), r = e - role * win.sinks * D;
+    if (role > 1 || r / D >= len) return;
+    const size_t slot = (size_t)nkv * 2 * win.sinks * D;
+    const float *src = part + (size_t)place * slot + (size_t)kvh * 2 * win.sinks * D + e;
+    f32x4 sum = *(const f32x4 *)src;
+    for (int c = 1; c < chunks; ++c) sum += *(const f32x4 *)(src + c * slot);
+    const float f = role ? scale : 1.f;
+    bf16x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = (__bf16)(sum[i] * f);
+    *(bf16x4 *)((role ? dk : dv) + (size_t)(ti.seg_start + r / D) * ldkv + kvh * D + r % D) = out;
+}
+
+// algorithmic forward FLOPs of a windowed launch: 4 nq d pairs (row, key it sees)
+double attn_window_flops(const ob_segments *seg, int nq, int d, int window, int sinks) {
+    double area = 0;
+    for (int j = 0; j < seg->n_seg; ++j) {
+        const double len = seg->cu_host[j + 1] - seg->cu_host[j], w = len < window ? len : window, past = len - w, s = sinks < w ? sinks : w;
+        area += w * (w + 1) / 2 + past * w;
+        // a row i >= w sees the sinks that have left its window: min(i + 1 - w, sinks)
+        area += past < s ? past * (past + 1) / 2 : s * (s + 1) / 2 + (past - s) * s;
+    }
+    return 4.0 * nq * d * area;
+}
+
 // algorithmic forward FLOPs: 4 nq d sum_seg A(s), A = s^2 or s (s + 1) / 2 (causal)
 double attn_flops(const ob_segments *seg, int nq, int d, bool causal) {
     double area = 0;
@@ -1497,11 +1639,11 @@ double attn_flops(const ob_segments *seg, int nq, int d, bool causal) {
 #define OB_ATTN_INSTANCES(D, C)                                                                               \
     template __global__ void attn_fwd_kernel<D, C>(const __bf16 *, const __bf16 *, const __bf16 *, __bf16 *,  \
                                                    float *, int, int, int, const int32_t *, int, int, int,    \
-                                                   float, int, TileOrder);                                    \
+                                                   float, int, TileOrder, Whole);                             \
     template __global__ void attn_bwd_dq_kernel<D, C>(const __bf16 *, const __bf16 *, const __bf16 *,         \
                                                       const __bf16 *, const __bf16 *, const float *, float *, \
                                                       float *, __bf16 *, int, int, int, const int32_t *, int, \
-                                                      int, int, float, float, int, TileOrder);                \
+                                                      int, int, float, float, int, TileOrder, Whole);         \
     OB_DKV_INSTANCE(D, C, dkv_np(D, 0), dkv_sr(D, 0))                                                         \
     OB_DKV_INSTANCE(D, C, dkv_np(D, 0), dkv_sr(D, 0), true)
 #define OB_DKV_INSTANCE(D, C, ...)                                                                                \
@@ -1509,7 +1651,7 @@ double attn_flops(const ob_segments *seg, int nq, int d, bool causal) {
                                                            const __bf16 *, const float *, const float *,      \
                                                            __bf16 *, __bf16 *, int, int, int,                 \
                                                            const int32_t *, int, int, int, float, float, int, \
-                                                           TileOrder);
+                                                           TileOrder, Whole);
 OB_ATTN_INSTANCES(64, true)
 OB_ATTN_INSTANCES(64, false)
 OB_DKV_INSTANCE(64, true, dkv_np(64, 1), dkv_sr(64, 1))
@@ -1523,7 +1665,29 @@ OB_ATTN_INSTANCES(128, false)
                                                            const __bf16 *, const float *, const float *,      \
                                                            __bf16 *, __bf16 *, int, int, int,                 \
                                                            const int32_t *, int, int, int, float, float, int, \
-                                                           TileOrder);
+                                                           TileOrder, Whole);
+#define OB_WINDOW_INSTANCES(D)                                                                                    \
+    template __global__ void attn_fwd_kernel<D, true, Band>(const __bf16 *, const __bf16 *, const __bf16 *, __bf16 *, \
+                                                            float *, int, int, int, const int32_t *, int, int, int, \
+                                                            float, int, TileOrder, Band);                          \
+    template __global__ void attn_bwd_dq_kernel<D, true, Band>(const __bf16 *, const __bf16 *, const __bf16 *,     \
+                                                               const __bf16 *, const __bf16 *, const float *,      \
+                                                               float *, float *, __bf16 *, int, int, int,          \
+                                                               const int32_t *, int, int, int, float, float, int,  \
+                                                               TileOrder, Band);                                   \
+    OB_WINDOW_DKV(D, Band, window_np(D), window_sr(D))                                                              \
+    OB_WINDOW_DKV(D, Sinks, 2, window_sr(D))                                                                        \
+    template __global__ void attn_sink_sum_kernel<D>(const float *, __bf16 *, __bf16 *, int, const int32_t *, int, Sinks, float);
+#define OB_WINDOW_DKV(D, W, NP, SR)                                                                               \
+    template __global__ void attn_bwd_dkv_kernel<D, true, NP, SR, false, W>(const __bf16 *, const __bf16 *, const __bf16 *, \
+                                                           const __bf16 *, const float *, const float *,      \
+                                                           __bf16 *, __bf16 *, int, int, int,                 \
+                                                           const int32_t *, int, int, int, float, float, int, \
+                                                           TileOrder, W);
+OB_WINDOW_INSTANCES(64)
+OB_WINDOW_INSTANCES(128)
+#undef OB_WINDOW_DKV
+#undef OB_WINDOW_INSTANCES
 OB_BLOCKS_INSTANCE(true)
 OB_BLOCKS_INSTANCE(false)
 #undef OB_BLOCKS_INSTANCE
@@ -1561,7 +1725,7 @@ void launch_attn_fwd(const void *q, const void *k, const void *v, void *o, float
     const dim3 grid((unsigned)tiles * nq);
     OB_ATTN_DISPATCH(attn_fwd_kernel, grid, 256, (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v,
                      (__bf16 *)o, lse, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, seg->total_tokens,
-                     nq / nkv, scale, nq, ord);
+                     nq / nkv, scale, nq, ord, Whole{});
 }
 
 void launch_attn_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
@@ -1579,7 +1743,7 @@ void launch_attn_bwd(const void *d_o, const void *q, const void *k, const void *
         const dim3 grid_q((unsigned)tiles * nq);
         OB_ATTN_DISPATCH(attn_bwd_dq_kernel, grid_q, 256, (const __bf16 *)d_o, (const __bf16 *)q,
                          (const __bf16 *)k, (const __bf16 *)v, (const __bf16 *)o, lse, lse2, delta, (__bf16 *)dq, ldq,
-                         ldkv, ldo, seg->cu_dev, seg->n_seg, seg->total_tokens, nq / nkv, scale, rot, nq, ord);
+                         ldkv, ldo, seg->cu_dev, seg->n_seg, seg->total_tokens, nq / nkv, scale, rot, nq, ord, Whole{});
     }
     ProfScope prof(K_ATTN_BWD_DKV, s, 1.5 * attn_flops(seg, nq, d, causal));  // dV, dP, dK
     TileOrder ord;
@@ -1590,7 +1754,7 @@ void launch_attn_bwd(const void *d_o, const void *q, const void *k, const void *
     const int kvt = 32 * dkv_np(d, shape), places = make_order(seg, kvt, causal, true, ord);
     const dim3 grid_kv((unsigned)places * nkv);
 #define OB_DKV_ARGS (const __bf16 *)d_o, (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, lse2, delta, (__bf16 *)dk,  \
-                    (__bf16 *)dv, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, group, scale, rot, nkv, ord
+                    (__bf16 *)dv, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, group, scale, rot, nkv, ord, Whole{}
     const int threads = dkv_threads(d, shape);
     if (apart) OB_ATTN_DISPATCH(attn_bwd_dkv_apart, grid_kv, threads, OB_DKV_ARGS);
     else if (shape == 0) OB_ATTN_DISPATCH(attn_bwd_dkv_0, grid_kv, threads, OB_DKV_ARGS);
@@ -1598,6 +1762,61 @@ void launch_attn_bwd(const void *d_o, const void *q, const void *k, const void *
     else if (d == 64) hipLaunchKernelGGL((attn_bwd_dkv<64, false, 2>), grid_kv, dim3(threads), 0, s, OB_DKV_ARGS);
     else hipLaunchKernelGGL((attn_bwd_dkv<128, false, 2>), grid_kv, dim3(threads), 0, s, OB_DKV_ARGS);
 #undef OB_DKV_ARGS
+}
+
+void launch_attn_window_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
+                            const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s) {
+    ProfScope prof(K_ATTN_FWD, s, attn_window_flops(seg, nq, d, window, sinks));
+    TileOrder ord;
+    const int tiles = make_order(seg, QT, true, false, ord, window);
+    const dim3 grid((unsigned)tiles * nq);
+#define OB_ARGS (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, (__bf16 *)o, lse, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, \
+                seg->total_tokens, nq / nkv, scale, nq, ord, Band{window, sinks}
+    if (d == 64) hipLaunchKernelGGL((attn_fwd_kernel<64, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
+    else hipLaunchKernelGGL((attn_fwd_kernel<128, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
+#undef OB_ARGS
+}
+
+// dQ; dK and dV of the keys that leave the window, by tiles of key rows; those of the sinks of segments longer than it, which every
+// row sees: a tile of key rows that walked all of a long segment would keep the launch waiting, so chunks of the queries leave
+// fp32 sums in `part` and a last launch adds them in order.
+void launch_attn_window_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
+                            float *lse2, float *delta, float *part, void *dq, void *dk, void *dv, int ldq, int ldkv, int ldo,
+                            const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s) {
+    const int T = seg->total_tokens, group = nq / nkv;
+    const double flops = attn_window_flops(seg, nq, d, window, sinks);
+    TileOrder ord;
+    {
+        ProfScope prof(K_ATTN_BWD_DQ, s, 0.5 * flops);
+        const int tiles = make_order(seg, QT, true, false, ord, window);
+        const dim3 grid((unsigned)tiles * nq);
+#define OB_ARGS (const __bf16 *)d_o, (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, (const __bf16 *)o, lse, lse2, delta,  \
+                (__bf16 *)dq, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, group, scale, 0.f, nq, ord, Band{window, sinks}
+        if (d == 64) hipLaunchKernelGGL((attn_bwd_dq_kernel<64, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
+        else hipLaunchKernelGGL((attn_bwd_dq_kernel<128, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
+#undef OB_ARGS
+    }
+    ProfScope prof(K_ATTN_BWD_DKV, s, 1.5 * flops);
+    const int places = make_order(seg, 32 * window_np(d), true, true, ord, window), threads = 128 * window_np(d);
+#define OB_ARGS(W) (const __bf16 *)d_o, (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, lse2, delta, (__bf16 *)dk, (__bf16 *)dv,  \
+                   ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, group, scale, 0.f, nkv, ord, W
+    const dim3 grid((unsigned)places * nkv);
+    const Band band{window, sinks};
+    if (d == 64) hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, window_np(64), window_sr(64), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
+    else hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, window_np(128), window_sr(128), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
+    const int chunks = sink_chunks(seg, window, sinks);
+    if (!chunks) return;
+    const Sinks first{window, sinks, sink_chunk_rows(window), part};
+    const dim3 grid_s((unsigned)chunks * nkv), grid_r(chunks, nkv, (2 * sinks * d + 1023) / 1024);
+    ord.n = 0;
+    if (d == 64) {
+        hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, 2, window_sr(64), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
+        hipLaunchKernelGGL((attn_sink_sum_kernel<64>), grid_r, dim3(256), 0, s, part, (__bf16 *)dk, (__bf16 *)dv, ldkv, seg->cu_dev, seg->n_seg, first, scale);
+    } else {
+        hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, 2, window_sr(128), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
+        hipLaunchKernelGGL((attn_sink_sum_kernel<128>), grid_r, dim3(256), 0, s, part, (__bf16 *)dk, (__bf16 *)dv, ldkv, seg->cu_dev, seg->n_seg, first, scale);
+    }
+#undef OB_ARGS
 }
 
 }  // namespace ob

@@ -25,7 +25,7 @@ int count_tiles(const ob_segments *seg, int tile_rows) {
 // the workgroup owns key rows and streams query tiles (from its diagonal on when causal); otherwise
 // it owns query rows and streams key tiles (up to its diagonal when causal).  A unit counts as its first
 // tile, on the key side the heaviest of them.  No heap memory.
-int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord) {
+int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window) {
     ord.n = ord.unit_log2 = 0;
     const int n_tiles = count_tiles(seg, tile_rows), max_log2 = kv_side && tile_rows == 64 ? 2 : 0;
     int log2 = 0, n_units = n_tiles;
@@ -42,6 +42,7 @@ int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side,
             int rows = len;                                            // streamed rows
             if (causal && kv_side) rows = len - (t * unit_rows) / ST * ST;
             else if (causal) rows = std::min(len, (t + 1) * unit_rows);
+            if (window) rows = std::min(rows, window + unit_rows);
             const uint32_t w = (uint32_t)((rows + ST - 1) / ST);
             // ascending sort of (~work, natural index); the entry rides in the low half
             key[n] = ((uint64_t)(0xFFFFFu - w) << 44) | ((uint64_t)n << 32) | ((uint32_t)j << 16) | (uint32_t)t;
@@ -53,6 +54,18 @@ int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side,
     ord.n = n;
     ord.unit_log2 = log2;
     return n << log2;
+}
+
+int sink_chunk_rows(int window) { return std::min(2048, std::max(256, (window + 64 + ST - 1) / ST * ST)); }
+int sink_chunks(const ob_segments *seg, int window, int sinks) {
+    if (!sinks) return 0;
+    const int rows = sink_chunk_rows(window);
+    int n = 0;
+    for (int j = 0; j < seg->n_seg; ++j) {
+        const int len = seg->cu_host[j + 1] - seg->cu_host[j];
+        if (len > window) n += (len + rows - 1) / rows;
+    }
+    return n;
 }
 
 // Which of its shapes dK / dV runs in (see the kernels).  An estimate of each shape's duration, to compare the shapes by and up to half as much again as the

@@ -48,7 +48,16 @@ __host__ __device__ constexpr bool dkv_tile_fits(uint32_t ld2, int sr) { return 
 __host__ __device__ constexpr uint32_t dkv_piece_offset(uint32_t voff, uint32_t row, uint32_t ld2) { return voff - row * ld2; }
 
 // the order of a launch; returns its places (workgroups per head): as many as tiles, or whole units of them
-int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord);
+// (window > 0: causal, a row sees no more than that many keys)
+int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window = 0);
 int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal);
+
+// Windowed attention: dK / dV in pairs of 32 key rows and query tiles, as above
+constexpr int window_np(int d) { return d == 64 ? 2 : 4; }
+constexpr int window_sr(int d) { return d == 64 ? 32 : 64; }
+// Rows of a chunk of queries that the sinks' sums are split into: about what a workgroup of the windowed launch walks, in whole tiles, and how
+// many such chunks the segments longer than the window have
+int sink_chunk_rows(int window);
+int sink_chunks(const ob_segments *seg, int window, int sinks);
 
 }  // namespace ob

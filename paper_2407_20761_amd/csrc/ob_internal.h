@@ -13,6 +13,8 @@ namespace ob {
 int fail(int status, const char *fmt, ...);
 int check_launch(const char *what);
 
+constexpr int MAX_TOKENS = 1 << 22;
+
 constexpr size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // host-side checks shared by the attention entry points (api.cpp); OB_OK or a status with the text set
@@ -119,6 +121,21 @@ void launch_attn_bwd(const void *d_o, const void *q, const void *k, const void *
                      const ob_segments *seg, int nq, int nkv, int d, float scale, int mask, float rotary_base,
                      hipStream_t s);
 
+// the same with a window and sinks (causal); part: sink_chunks() x nkv x 2 x sinks x d floats
+void launch_attn_window_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
+                            const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s);
+void launch_attn_window_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
+                            float *lse2, float *delta, float *part, void *dq, void *dk, void *dv, int ldq, int ldkv, int ldo,
+                            const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s);
+
+// ---- rotary positions with several axes (rotary_axes.hip) ----------------------------------------
+// per pair of a head: the fraction of a turn per position, in units of 2^-64, and the axis (-1: the pair passes)
+struct RotaryTable { uint64_t turn[64]; int8_t axis[64]; };
+// checks the description and fills the table
+int rotary_table(const ob_rotary_axes_desc *desc, RotaryTable &table, const char *who);
+void launch_rotary_axes(const void *x, int ldx, void *y, int ldy, int T, int n_heads, int d, const RotaryTable &table,
+                        const int32_t *pos, int inverse, int dtype, hipStream_t s);
+
 // ---- fp32 debug path (debug_fp32.hip): every tensor fp32, plain FMA kernels --------------------
 namespace f32 {
 struct SavedF32 { size_t h1, qkv, o, lse, x1, h2, up, act, stat1, stat2, total; };
@@ -131,6 +148,11 @@ void attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse, 
 void attn_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
               void *dq, void *dk, void *dv, float *delta, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
               int nkv, int d, float scale, int mask, hipStream_t s);
+void attn_window_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
+                     const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s);
+void attn_window_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
+                     void *dq, void *dk, void *dv, float *delta, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
+                     int nkv, int d, float scale, int window, int sinks, hipStream_t s);
 void block_fwd(const ob_block_desc *dsc, const ob_block_weights *w, const void *x, void *y, void *saved,
                const ob_segments *seg, hipStream_t s);
 void block_bwd(const ob_block_desc *dsc, const ob_block_weights *w, const ob_block_grads *g, int accumulate,
