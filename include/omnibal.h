@@ -264,6 +264,32 @@ int ob_connector_bwd(const ob_connector_desc *desc, const ob_connector_weights *
                      const int32_t *dst_rows_dev, int llm_tokens, const void *saved,
                      size_t saved_bytes, void *ws, size_t ws_bytes, void *hip_stream);
 
+/* ---- softmax cross entropy over a vocabulary ------------------------------------------------------
+ * The end of the language model: logits z = x_r W^T of the supervised rows of x, lse_r = log sum_v exp z_rv,
+ * nll_r = lse_r - z_r,label, and for the gradients dnll_r of the losses
+ *   G_rv = (exp(z_rv - lse_r) - [v = label_r]) dnll_r,   dx_r = sum_v G_rv W_v,   dW_v = sum_r G_rv x_r
+ * The logits are never stored: the forward reduces each tile of them where it is computed, the backward computes them again
+ * a piece of the vocabulary at a time (at most 1 GiB of G in bf16; fp32 sums of dx over the pieces, added in order).  No
+ * atomics: results are bitwise reproducible.
+ * x [total_tokens, hidden], w [vocab, hidden].  rows (int32, n_rows entries, host and device copies): the supervised rows,
+ * ascending, checked on the host; both NULL: every row (n_rows = total_tokens).  Visual tokens and prompts have no label, so a
+ * packed batch has far fewer rows here than tokens.  labels, nll, lse, dnll: device memory, n_rows entries.  A row whose label is
+ * outside [0, vocab) is ignored: nll 0, no gradient whatever its dnll (x of a listed row has to be finite).
+ * ob_lm_loss_bwd, given lse of the forward, writes every row of dx (rows not listed: zeros) and dw (flags: OB_BWD_ACCUMULATE
+ * adds to dw).  ws (ob_lm_loss_workspace_bytes) need not be kept between the two.  dtype OB_BF16, or OB_FP32 for the debug variant (x,
+ * w, dx, dw fp32; plain kernels); hidden a multiple of 64 up to 8192, vocab up to 2^21, tensors and ws aligned to 16 bytes. */
+typedef struct {
+    int hidden, vocab;
+    int dtype;         /* ob_dtype */
+} ob_lm_loss_desc;
+size_t ob_lm_loss_workspace_bytes(const ob_lm_loss_desc *desc, int n_rows);
+int ob_lm_loss_fwd(const ob_lm_loss_desc *desc, const void *w, const void *x, int total_tokens, const int32_t *rows_host,
+                   const int32_t *rows_dev, int n_rows, const int32_t *labels, float *nll, float *lse, void *ws, size_t ws_bytes,
+                   void *hip_stream);
+int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void *w, const void *x, int total_tokens, const int32_t *rows_host,
+                   const int32_t *rows_dev, int n_rows, const int32_t *labels, const float *lse, const float *dnll, void *dx,
+                   void *dw, void *ws, size_t ws_bytes, void *hip_stream);
+
 /* ---- rotary positions with several axes ---------------------------------------------------------
  * The blocks above turn by a token's distance to the start of its segment.  Image and video tokens have a place along several
  * axes (time, height, width): here pair i of a head, its elements (i, i + d/2), turns by a = pos[axis_of_pair[i]][t] theta_i:

@@ -60,6 +60,10 @@ class ob_attn_bwd_launch(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("key_rows", "query_rows", "workgroups", "order_rows")]
 
 
+class ob_lm_loss_desc(C.Structure):
+    _fields_ = [("hidden", C.c_int), ("vocab", C.c_int), ("dtype", C.c_int)]
+
+
 class ob_rotary_axes_desc(C.Structure):
     _fields_ = [("head_dim", C.c_int), ("n_axes", C.c_int), ("base", C.c_float), ("per_axis", C.c_int), ("axis_of_pair", C.c_int8 * 64)]
 
@@ -124,6 +128,9 @@ _SIGNATURES = {
     "ob_gemm_act_plan": (_I, [_I, _I, _I, _I, _I, _I, C.POINTER(ob_gemm_launch), C.POINTER(C.c_int)]),
     "ob_varlen_attn_bwd_plan": (_I, [_SEG, _I, _I, _I, _I, C.POINTER(ob_attn_bwd_launch), _i32p, _I]),
     "ob_varlen_attn_bwd_threads": (_I, [_SEG, _I, _I, _I, _I, C.POINTER(C.c_int)]),
+    "ob_lm_loss_workspace_bytes": (_Z, [C.POINTER(ob_lm_loss_desc), _I]),
+    "ob_lm_loss_fwd": (_I, [C.POINTER(ob_lm_loss_desc), _P, _P, _I, _P, _P, _I, _P, _P, _P, _P, _Z, _P]),
+    "ob_lm_loss_bwd": (_I, [C.POINTER(ob_lm_loss_desc), _I, _P, _P, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "ob_rotary_axes": (_I, [C.POINTER(ob_rotary_axes_desc), _P, _I, _P, _I, _I, _I, _P, _I, _I, _P]),
     "ob_debug_materialize_mask": (_I, [_SEG, _I, _P, _P]),
     "ob_connector_saved_bytes": (_Z, [C.POINTER(ob_connector_desc), _I]),
@@ -391,6 +398,29 @@ def ob_connector_bwd(desc, weights: dict, grads: dict, flags, v, dx_llm, dv, n_t
     _check(lib.ob_connector_bwd(C.byref(desc), C.byref(w), C.byref(g), int(flags), _ptr(v), _ptr(dx_llm),
                                 _ptr(dv), n_tiles, dst_rows.host_ptr, _ptr(dst_rows.dev), llm_tokens,
                                 _ptr(saved), _nbytes(saved), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def make_lm_loss_desc(hidden, vocab, dtype=OB_BF16) -> ob_lm_loss_desc:
+    return ob_lm_loss_desc(int(hidden), int(vocab), dtype)
+
+
+def ob_lm_loss_workspace_bytes(desc, n_rows) -> int:
+    return lib.ob_lm_loss_workspace_bytes(C.byref(desc), n_rows)
+
+
+def _row_list(rows, total_tokens):
+    """host pointer, device pointer and length of a RowIndex; None: all rows"""
+    return (None, None, total_tokens) if rows is None else (rows.host.ctypes.data, rows.dev.data_ptr(), len(rows.host))
+
+
+def ob_lm_loss_fwd(desc, w, x, total_tokens, rows: RowIndex | None, labels, nll, lse, ws, stream=None):
+    _check(lib.ob_lm_loss_fwd(C.byref(desc), _ptr(w), _ptr(x), total_tokens, *_row_list(rows, total_tokens), _ptr(labels), _ptr(nll), _ptr(lse),
+                              _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def ob_lm_loss_bwd(desc, flags, w, x, total_tokens, rows: RowIndex | None, labels, lse, dnll, dx, dw, ws, stream=None):
+    _check(lib.ob_lm_loss_bwd(C.byref(desc), int(flags), _ptr(w), _ptr(x), total_tokens, *_row_list(rows, total_tokens), _ptr(labels), _ptr(lse),
+                              _ptr(dnll), _ptr(dx), _ptr(dw), _ptr(ws), _nbytes(ws), _stream(stream)))
 
 
 def make_rotary_axes_desc(axis_of_pair, head_dim, base=10000.0, per_axis=False) -> ob_rotary_axes_desc:

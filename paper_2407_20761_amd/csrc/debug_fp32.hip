@@ -604,5 +604,93 @@ void connector_bwd(const ob_connector_weights *w, const ob_connector_grads *gr, 
     hipLaunchKernelGGL(subsample_scatter_kernel, dim3(blocks_for(n_dv)), dim3(256), 0, s, du, OB_FM(dv), n_dv, g, Hv);
 }
 
+// ---- cross entropy over a vocabulary, fp32: logits of a few rows at a time -----------------------
+// one workgroup to a row of z [n, V]; GRAD: z becomes (softmax - one-hot) weight
+template <bool GRAD>
+__global__ __launch_bounds__(256) void loss_row_kernel(float *__restrict__ z, int V, const int32_t *__restrict__ labels, float *__restrict__ nll,
+                                                       float *__restrict__ lse, const float *__restrict__ dnll) {
+    __shared__ float sh[4];
+    const int row = blockIdx.x, label = labels[row];
+    float *const p = z + (size_t)row * V;
+    const bool has = label >= 0 && label < V;
+    if (GRAD) {
+        const float weight = has ? dnll[row] : 0.f, l = lse[row];
+        for (int i = threadIdx.x; i < V; i += 256) p[i] = weight == 0.f ? 0.f : (expf(p[i] - l) - (i == label ? 1.f : 0.f)) * weight;
+        return;
+    }
+    float mx = -INFINITY, sum = 0.f;
+    for (int i = threadIdx.x; i < V; i += 256) mx = fmaxf(mx, p[i]);
+    for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+    for (int i = threadIdx.x; i < V; i += 256) sum += expf(p[i] - mx);
+    const float l = mx + logf(block_sum(sum, sh));
+    if (threadIdx.x == 0) {
+        lse[row] = l;
+        nll[row] = has ? l - p[label] : 0.f;
+    }
+}
+// big[t] = small[i] where rows[i] = t (ascending), else zeros
+__global__ __launch_bounds__(256) void rows_spread_kernel(const float *__restrict__ small, float *__restrict__ big, const int32_t *__restrict__ rows,
+                                                          int n_rows, int H) {
+    const int t = blockIdx.x;
+    int lo = 0, hi = n_rows;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (rows[mid] < t) lo = mid + 1; else hi = mid;
+    }
+    const bool listed = lo < n_rows && rows[lo] == t;
+    for (int c = threadIdx.x; c < H; c += 256) big[(size_t)t * H + c] = listed ? small[(size_t)lo * H + c] : 0.f;
+}
+
+struct LossWork { size_t xs, dxs, z, total; int rows; };
+static LossWork loss_work(int n, int H, int V) {
+    LossWork w; size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off += up256(bytes); return o; };
+    const int fit = (1 << 24) / V;      // 64 MB of logits
+    w.rows = fit < 1 ? 1 : fit < n ? fit : n;
+    w.xs = take((size_t)n * H * 4); w.dxs = take((size_t)n * H * 4); w.z = take((size_t)w.rows * V * 4);
+    w.total = off;
+    return w;
+}
+size_t lm_loss_work_bytes(int n, int H, int V) { return loss_work(n, H, V).total; }
+
+static const float *loss_rows(const void *x, const int32_t *rows_dev, int n, int H, const LossWork &wk, unsigned char *ws, hipStream_t s) {
+    if (!rows_dev) return OB_F(x);
+    hipLaunchKernelGGL(rows_copy_kernel, dim3(blocks_for((long)n * H)), dim3(256), 0, s, OB_FM(ws + wk.xs), (float *)x /* read only */, rows_dev,
+                       (long)n * H, H, 0);
+    return OB_F(ws + wk.xs);
+}
+
+void lm_loss_fwd(const void *w, const void *x, const int32_t *rows_dev, int n, int H, int V, const int32_t *labels, float *nll, float *lse,
+                 void *ws, hipStream_t s) {
+    const LossWork wk = loss_work(n, H, V);
+    const float *xs = loss_rows(x, rows_dev, n, H, wk, (unsigned char *)ws, s);
+    float *z = OB_FM((unsigned char *)ws + wk.z);
+    for (int i = 0; i < n; i += wk.rows) {
+        const int m = n - i < wk.rows ? n - i : wk.rows;
+        gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, nullptr, nullptr, 0, s);
+        hipLaunchKernelGGL((loss_row_kernel<false>), dim3(m), dim3(256), 0, s, z, V, labels + i, nll + i, lse + i, (const float *)nullptr);
+    }
+}
+
+void lm_loss_bwd(const void *w, const void *x, int T, const int32_t *rows_dev, int n, int H, int V, const int32_t *labels, const float *lse,
+                 const float *dnll, void *dx, void *dw, int accumulate, void *ws, hipStream_t s) {
+    const LossWork wk = loss_work(n, H, V);
+    unsigned char *wb = (unsigned char *)ws;
+    const float *xs = loss_rows(x, rows_dev, n, H, wk, wb, s);
+    float *z = OB_FM(wb + wk.z), *dxs = rows_dev ? OB_FM(wb + wk.dxs) : OB_FM(dx);
+    for (int i = 0; i < n; i += wk.rows) {
+        const int m = n - i < wk.rows ? n - i : wk.rows;
+        gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, nullptr, nullptr, 0, s);
+        hipLaunchKernelGGL((loss_row_kernel<true>), dim3(m), dim3(256), 0, s, z, V, labels + i, (float *)nullptr, (float *)lse + i /* read only */,
+                           dnll + i);
+        gemm(2, V, H, m, z, xs + (size_t)i * H, OB_FM(dw), nullptr, nullptr, accumulate || i > 0 ? 1 : 0, s);
+        gemm(1, m, H, V, z, OB_F(w), dxs + (size_t)i * H, nullptr, nullptr, 0, s);
+    }
+    if (rows_dev) hipLaunchKernelGGL(rows_spread_kernel, dim3(T), dim3(256), 0, s, dxs, OB_FM(dx), rows_dev, n, H);
+}
+
 }  // namespace f32
 }  // namespace ob

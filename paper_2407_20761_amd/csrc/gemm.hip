@@ -529,7 +529,51 @@ struct KLoop {
 //   EPI_GELU_BWD    C = x GELU'(up), up in place of R
 //   EPI_SWIGLU_BWD  C[m, n], C[m, N + n]: the gradients of gate and up for x, that of their product; up [M, 2 N] in place of R
 // The last two leave the fp32 sums of each half tile's columns of C at colsum[2 tile_m + wave row][C's columns] (may be null: in place of the bias).
-enum { EPI_PLAIN = 0, EPI_ROWS, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD };
+// The last two are those of the cross entropy over a vocabulary, whose logits z = x W^T ("NT") are not stored:
+//   EPI_LOSS_STATS  per row of z and column half of a tile its maximum and the sum of exp(z - maximum): float2 [2 tiles_n][M] in place of C; the logit of
+//                   the row's label (in place of R) to float [M] in place of the bias, by the lane that holds it
+//   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) weight, zeros in the columns N .. ldc; LossRow [M] in place of R, ldr the label of column 0
+enum { EPI_PLAIN = 0, EPI_ROWS, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD, EPI_LOSS_STATS, EPI_LOSS_GRAD };
+constexpr float LOG2E = 1.4426950408889634f;
+
+// EPI_LOSS_STATS, straight from the accumulators: a lane holds, of rows 16 i + lane % 16, columns 16 j + 4 (lane / 16) .. + 3 of the wave's part, so a
+// row's maximum and sum are the lane's own and two exchanges with the lanes of the same row.
+template <int TA, int TB>
+__device__ __forceinline__ void loss_stats(const f32x4 (&acc)[TA][TB], int M, int N, int m0, int c0, float2 *__restrict__ stats,
+                                           float *__restrict__ target, const int32_t *__restrict__ labels) {
+    const int lane = threadIdx.x & 63, lx = lane & 15, lq = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < TA; ++i) {
+        const int m = m0 + 16 * i + lx;
+        float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, c0 + 16 * j + 4 * lq + r < N ? acc[i][j][r] : -INFINITY);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float c = mx == -INFINITY ? 0.f : mx * LOG2E;      // (a part past the last column)
+#pragma unroll
+        for (int j = 0; j < TB; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                sum += c0 + 16 * j + 4 * lq + r < N ? __builtin_amdgcn_exp2f(acc[i][j][r] * LOG2E - c) : 0.f;
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (m < M && lq == 0) stats[m] = float2{mx, sum};
+        const int label = m < M ? labels[m] : -1, rel = label - c0;
+        const bool hit = rel >= 0 && rel < 16 * TB && label < N && ((rel >> 2) & 3) == lq;
+        if (__any(hit)) {
+            float z = 0.f;
+#pragma unroll
+            for (int j = 0; j < TB; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) z = rel == 16 * j + 4 * lq + r ? acc[i][j][r] : z;
+            if (hit) target[m] = z;
+        }
+    }
+}
+
 template <int BM, int BN, int WM, int WN, bool AK, bool BKM, int NS, int EPI = EPI_PLAIN>
 __device__ __forceinline__ void gemm_tile(
     int M, int N, int K, const __bf16 *__restrict__ A, int lda, const __bf16 *__restrict__ B,
@@ -613,6 +657,11 @@ __device__ __forceinline__ void gemm_tile(
     __builtin_amdgcn_s_waitcnt(waitcnt(0, 0));
     __syncthreads();
     constexpr int CW = BN / WN;            // columns of the wave's tile
+    if constexpr (EPI == EPI_LOSS_STATS) {
+        loss_stats<TA, TB>(acc, M, N, m0 + wm * (BM / WM), n0 + wn * CW, (float2 *)Cm + (size_t)(WN * tile_n + wn) * M, (float *)bias,
+                           (const int32_t *)side);
+        return;
+    }
     constexpr int RSTR = CW * 4 + 16;      // fp32 row stride in LDS, padded against bank conflicts
     constexpr int LPR = CW / 8;            // lanes per row on the way out (8 columns each)
     constexpr int RPI = 64 / LPR;          // rows per read instruction
@@ -635,6 +684,37 @@ __device__ __forceinline__ void gemm_tile(
             for (int j = 0; j < TB; ++j)
                 *(f32x4 OB_LDS *)(slab + (16 * h + lx) * RSTR + (j * 16 + lq * 4) * 4) = acc[2 * ii + h][j];
     };
+    if constexpr (EPI == EPI_LOSS_GRAD) {
+        put(0);
+#pragma unroll
+        for (int ii = 0; ii < TA / 2; ++ii) {
+            constexpr int NR = 32 / RPI;
+            f32x4 lo[NR], hi[NR];
+            LossRow of[NR];
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int row = r * RPI + lane / LPR, m = m0 + wm * (BM / WM) + ii * 32 + row;
+                lo[r] = *(const f32x4 OB_LDS *)(slab + row * RSTR + (lane % LPR) * 32);
+                hi[r] = *(const f32x4 OB_LDS *)(slab + row * RSTR + (lane % LPR) * 32 + 16);
+                of[r] = m < M ? ((const LossRow *)side)[m] : LossRow{0.f, 0.f, -1, 0};
+            }
+            if (ii + 1 < TA / 2) put(ii + 1);
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int m = m0 + wm * (BM / WM) + ii * 32 + r * RPI + lane / LPR, rel = of[r].label - ldr - n_out;
+                bf16x8 g;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float z = e < 4 ? lo[r][e & 3] : hi[r][e & 3];
+                    // (a row without a label has weight 0: its logits may be anything)
+                    const float p = __builtin_amdgcn_exp2f(z * LOG2E - of[r].lse2) - (e == rel ? 1.f : 0.f);
+                    g[e] = (__bf16)(of[r].weight == 0.f || n_out + e >= N ? 0.f : p * of[r].weight);
+                }
+                if (m < M && n_out < ldc) *(bf16x8 *)(Cm + (size_t)m * ldc + n_out) = g;
+            }
+        }
+        return;
+    }
     float cs[2][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) cs[0][e] = cs[1][e] = 0.f;
@@ -734,7 +814,8 @@ __device__ __forceinline__ void gemm_tile(
     };
     using std::integral_constant;
     const bool inside = m0 + BM <= M && n0 + BN <= N;
-    if constexpr (EPI >= EPI_GELU) {
+    if constexpr (EPI >= EPI_LOSS_STATS) return;      // (above)
+    else if constexpr (EPI >= EPI_GELU) {
         if (inside) out(integral_constant<int, 0>{}, integral_constant<bool, false>{});
         else out(integral_constant<int, 0>{}, integral_constant<bool, true>{});
         if constexpr (EPI >= EPI_GELU_BWD) {
@@ -756,9 +837,8 @@ __device__ __forceinline__ void gemm_tile(
                 }
             }
         }
-        return;
     }
-    if (sliced) out(integral_constant<int, 2>{}, integral_constant<bool, false>{});
+    else if (sliced) out(integral_constant<int, 2>{}, integral_constant<bool, false>{});
     else if (inside && R) out(integral_constant<int, 1>{}, integral_constant<bool, false>{});
     else if (inside) out(integral_constant<int, 0>{}, integral_constant<bool, false>{});
     else if (R) out(integral_constant<int, 1>{}, integral_constant<bool, true>{});
@@ -849,6 +929,12 @@ OB_GEMM_INSTANCE(128, 128, false, true, 4, EPI_GELU_BWD)
 OB_GEMM_INSTANCE(64, 64, false, true, 8, EPI_GELU_BWD)
 OB_GEMM_INSTANCE(128, 128, false, true, 4, EPI_SWIGLU_BWD)
 OB_GEMM_INSTANCE(64, 64, false, true, 8, EPI_SWIGLU_BWD)
+OB_GEMM_INSTANCE(256, 256, false, false, 4, EPI_LOSS_STATS)
+OB_GEMM_INSTANCE(128, 128, false, false, 4, EPI_LOSS_STATS)
+OB_GEMM_INSTANCE(64, 64, false, false, 8, EPI_LOSS_STATS)
+OB_GEMM_INSTANCE(256, 256, false, false, 4, EPI_LOSS_GRAD)
+OB_GEMM_INSTANCE(128, 128, false, false, 4, EPI_LOSS_GRAD)
+OB_GEMM_INSTANCE(64, 64, false, false, 8, EPI_LOSS_GRAD)
 #undef OB_GEMM_INSTANCE
 template <class... A>
 constexpr size_t arg_bytes(void (*)(A...)) {
@@ -1071,6 +1157,70 @@ int gemm_any(int layout, int M, int N, int K, const void *A, const void *B, void
     else
         launch_layout<true, true>(2, M, N, K, A, M, B, N, C, N, bias, R, N, part, s);
     return check_launch("gemm");
+}
+
+// ---- cross entropy over a vocabulary ----------------------------------------------------------------
+// z = A B^T, [M, N] over K, in whole tiles of p (loss_plan), in pieces of the columns where the caller cuts B
+template <int EPI>
+static void launch_loss(const Plan &p, int M, int N, int K, const void *A, const void *B, void *C, int ldc, const void *bias, const void *side,
+                        int ldr, hipStream_t s) {
+    ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
+    const TailSplit ts{nullptr, 0, 0, 1, 0};
+    const int tm = (M + tile_rows(p.kind) - 1) / tile_rows(p.kind), tn = (N + tile_cols(p.kind) - 1) / tile_cols(p.kind);
+#define OB_ARGS dim3(tm * tn), dim3(256), 0, s, M, N, K, (const __bf16 *)A, K, (const __bf16 *)B, K, (__bf16 *)C, ldc, (const __bf16 *)bias,  \
+                (const __bf16 *)side, ldr, tm, tn, ts
+    if (p.kind == BIG) hipLaunchKernelGGL((gemm_kernel<256, 256, 2, 2, false, false, 4, EPI>), OB_ARGS);
+    else if (p.kind == SMALL) hipLaunchKernelGGL((gemm_kernel<128, 128, 2, 2, false, false, 4, EPI>), OB_ARGS);
+    else hipLaunchKernelGGL((gemm_kernel<64, 64, 2, 2, false, false, 8, EPI>), OB_ARGS);
+#undef OB_ARGS
+}
+void launch_loss_stats(const Plan &p, int n, int V, int H, const void *x, const void *w, const int32_t *labels, void *stats, float *target,
+                       hipStream_t s) {
+    launch_loss<EPI_LOSS_STATS>(p, n, V, H, x, w, stats, 0, target, labels, 0, s);
+}
+void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, const void *w, const LossRow *rows, int first, void *g, int ldg,
+                      hipStream_t s) {
+    launch_loss<EPI_LOSS_GRAD>(p, n, cols, H, x, w, g, ldg, nullptr, rows, first, s);
+}
+
+// "NN" and "TN" with operands whose rows are longer than the product's; ws: as for gemm_any()
+void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *B, void *C, void *ws, size_t ws_bytes, hipStream_t s) {
+    ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
+    float *part = ws && ws_bytes >= gemm_workspace_bytes(1, M, N, K) ? (float *)ws : nullptr;
+    launch_layout<false, true>(1, M, N, K, A, lda, B, N, C, N, nullptr, nullptr, 0, part, s);
+}
+void launch_gemm_tn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *R, hipStream_t s) {
+    ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
+    launch_layout<true, true>(2, M, N, K, A, lda, B, N, C, N, nullptr, R, N, nullptr, s);
+}
+
+// An "NN" product whose contraction comes in pieces that are not in memory at one time: piece after piece leaves fp32 sums of all its tiles, like the
+// slices of a split contraction, and the last launch adds them in order.
+template <int BM, int BN, int NS>
+static void nn_piece(int M, int N, int K, const void *A, int lda, const void *B, float *part, int index, hipStream_t s) {
+    const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
+    const TailSplit ts{part + (size_t)index * tm * tn * (BM * BN), 0, tm * tn, 1, (K + KSTEP - 1) / KSTEP};
+    hipLaunchKernelGGL((gemm_kernel<BM, BN, 2, 2, false, true, NS>), dim3(tm * tn), dim3(256), 0, s, M, N, K, (const __bf16 *)A, lda,
+                       (const __bf16 *)B, N, (__bf16 *)nullptr, N, (const __bf16 *)nullptr, (const __bf16 *)nullptr, 0, tm, tn, ts);
+}
+template <int BM, int BN>
+static void nn_sum(int M, int N, float *part, int pieces, void *C, hipStream_t s) {
+    const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
+    const TailSplit ts{part, 0, tm * tn, pieces, 0};
+    hipLaunchKernelGGL((tail_sum_kernel<BM, BN>), dim3(tm * tn * (BM * BN / 8 / 256)), dim3(256), 0, s, ts, M, N, tm, tn,
+                       (const __bf16 *)nullptr, (const __bf16 *)nullptr, 0, (__bf16 *)C, N, (const int32_t *)nullptr);
+}
+void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, int index, hipStream_t s) {
+    ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
+    if (p.kind == BIG) nn_piece<256, 256, 4>(M, N, K, A, lda, B, part, index, s);
+    else if (p.kind == SMALL) nn_piece<128, 128, 4>(M, N, K, A, lda, B, part, index, s);
+    else nn_piece<64, 64, 8>(M, N, K, A, lda, B, part, index, s);
+}
+void launch_gemm_nn_sum(const Plan &p, int M, int N, float *part, int pieces, void *C, hipStream_t s) {
+    ProfScope prof(K_REDUCE, s, 4.0 * M * N * pieces + 2.0 * M * N);
+    if (p.kind == BIG) nn_sum<256, 256>(M, N, part, pieces, C, s);
+    else if (p.kind == SMALL) nn_sum<128, 128>(M, N, part, pieces, C, s);
+    else nn_sum<64, 64>(M, N, part, pieces, C, s);
 }
 
 }  // namespace ob

@@ -175,6 +175,18 @@ Plan make_plan(int layout, int M, int N, int K, size_t scratch, bool cold, doubl
 
 }  // namespace
 
+Plan whole_plan(int layout, int M, int N, int K) {
+    const int nk = (K + KSTEP - 1) / KSTEP;
+    Plan best{};
+    double t_best = 0;
+    for (TileKind kind : {BIG, SMALL, FINE}) {
+        const Plan p{kind, tiles_of(kind, M, N), 0, 1, 0};
+        const double t = estimate_us(layout, kind, nk, bytes_of(M, N, K), p);
+        if (kind == BIG || t < t_best) { t_best = t; best = p; }
+    }
+    return best;
+}
+
 // Rows of a GEMM whose big (or 192-row) tiles fill whole rounds, and the rest as a launch of its own with the tiles
 // that suit it.  A row of tiles that spills over a round costs the chip a round: 12300 rows are 48 rows of tiles and
 // twelve rows of values, 16 tiles more than three rounds of 4096 columns (over K = 1024 104 us, cut 93; the 557 rows of

@@ -34,6 +34,8 @@ int tiles_of(TileKind kind, int M, int N);
 size_t scratch_bytes(int M, int N, int K);
 // the launches of a GEMM; layout 0 "NT", 1 "NN", 2 "TN"; `scratch`: bytes for slice sums
 RowCut make_row_cut(int layout, int M, int N, int K, size_t scratch);
+// whole tiles, one launch, of one of three kinds: BIG, SMALL or FINE
+Plan whole_plan(int layout, int M, int N, int K);
 // GEMMs with an activation in the epilogue: layouts of gemm_any() beyond the three (internal).  Whether such a launch is taken instead of two, and its
 // plan; `scratch`: the GEMM alone would have room for slice sums
 enum { GEMM_NT_GELU = 3, GEMM_NN_GELU_BWD = 4, GEMM_NN_SWIGLU_BWD = 5 };

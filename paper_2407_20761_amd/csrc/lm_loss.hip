@@ -1,0 +1,90 @@
+// Row kernels of the cross entropy over a vocabulary: what stands between its matrix products (gemm.hip).
+//   lse_r = log sum_v exp z_rv from the maxima and sums of the vocabulary's parts;  nll_r = lse_r - z_r,label
+// All are bound by memory and small beside the products.
+#include <cmath>
+
+#include "ob_internal.h"
+
+namespace ob {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+// sums of exp(z - m) of two parts, as one
+__device__ __forceinline__ void join(float &m, float &sum, float m2, float sum2) {
+    if (sum2 == 0.f) return;                       // (a part without columns: its maximum is -infinity)
+    const float top = fmaxf(m, m2);
+    sum = (sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((m - top) * LOG2E)) + sum2 * __builtin_amdgcn_exp2f((m2 - top) * LOG2E);
+    m = top;
+}
+
+// 16 rows to a workgroup, 16 threads to a row, each every sixteenth part; stats [slots][n], so the rows of a part are read together
+__global__ __launch_bounds__(256) void loss_combine_kernel(const float2 *__restrict__ stats, const float *__restrict__ target,
+                                                           const int32_t *__restrict__ labels, int n, int V, int slots,
+                                                           float *__restrict__ nll, float *__restrict__ lse) {
+    __shared__ float2 sh[16][17];
+    const int row = blockIdx.x * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
+    float m = -INFINITY, sum = 0.f;
+    if (row < n) {
+#pragma unroll 4
+        for (int i = lane; i < slots; i += 16) {
+            const float2 p = stats[(size_t)i * n + row];
+            join(m, sum, p.x, p.y);
+        }
+    }
+    sh[lane][threadIdx.x & 15] = float2{m, sum};
+    __syncthreads();
+    if (lane != 0 || row >= n) return;
+    for (int i = 1; i < 16; ++i) join(m, sum, sh[i][threadIdx.x].x, sh[i][threadIdx.x].y);
+    const float l = m + logf(sum);
+    const int label = labels[row];
+    lse[row] = l;
+    nll[row] = label >= 0 && label < V ? l - target[row] : 0.f;
+}
+
+__global__ __launch_bounds__(256) void loss_rows_kernel(const float *__restrict__ lse, const float *__restrict__ dnll,
+                                                        const int32_t *__restrict__ labels, int n, int V, LossRow *__restrict__ rows) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int label = labels[i];
+    rows[i] = LossRow{lse[i] * LOG2E, label >= 0 && label < V ? dnll[i] : 0.f, label, 0};
+}
+
+// one wave to a row of `big`: its place in the list by bisection
+__global__ __launch_bounds__(256) void rows_spread_kernel(const __bf16 *__restrict__ small, __bf16 *__restrict__ big,
+                                                          const int32_t *__restrict__ rows, int n_rows, int T, int H) {
+    const int t = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= T) return;
+    int lo = 0, hi = n_rows;                       // the first row of the list that is not below t
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (rows[mid] < t) lo = mid + 1; else hi = mid;
+    }
+    const bool listed = lo < n_rows && rows[lo] == t;
+    for (int c = (threadIdx.x & 63) * 8; c < H; c += 512) {
+        bf16x8 v = {};
+        if (listed) v = *(const bf16x8 *)(small + (size_t)lo * H + c);
+        *(bf16x8 *)(big + (size_t)t * H + c) = v;
+    }
+}
+
+}  // namespace
+
+void launch_loss_combine(const void *stats, const float *target, const int32_t *labels, int n, int V, int slots, float *nll, float *lse,
+                         hipStream_t s) {
+    ProfScope prof(K_REDUCE, s, 8.0 * n * slots);
+    hipLaunchKernelGGL(loss_combine_kernel, dim3((n + 15) / 16), dim3(256), 0, s, (const float2 *)stats, target, labels, n, V, slots, nll, lse);
+}
+void launch_loss_rows(const float *lse, const float *dnll, const int32_t *labels, int n, int V, LossRow *rows, hipStream_t s) {
+    ProfScope prof(K_ROWS, s, 28.0 * n);
+    hipLaunchKernelGGL(loss_rows_kernel, dim3((n + 255) / 256), dim3(256), 0, s, lse, dnll, labels, n, V, rows);
+}
+void launch_rows_spread(const void *small, void *big, const int32_t *rows_dev, int n_rows, int T, int H, hipStream_t s) {
+    ProfScope prof(K_ROWS, s, 2.0 * H * ((double)T + n_rows));
+    hipLaunchKernelGGL(rows_spread_kernel, dim3((T + 3) / 4), dim3(256), 0, s, (const __bf16 *)small, (__bf16 *)big, rows_dev, n_rows, T, H);
+}
+
+}  // namespace ob

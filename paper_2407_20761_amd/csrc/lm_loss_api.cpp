@@ -1,0 +1,165 @@
+// C ABI of the cross entropy over a vocabulary: validation, the pieces of the vocabulary, and its forward and backward out of the matrix
+// products (gemm.hip) and row kernels (lm_loss.hip).
+#include "gemm_plan.h"
+#include "ob_internal.h"
+
+using namespace ob;
+
+namespace {
+
+constexpr int MAX_HIDDEN = 8192, MAX_VOCAB = 1 << 21;
+// Bytes that the gradient of the logits, in bf16, may take at a time
+constexpr size_t PIECE_BYTES = (size_t)1 << 30;
+
+struct Bump {
+    size_t off = 0;
+    size_t take(size_t bytes) { const size_t o = off; off += align_up(bytes, 256); return o; }
+};
+
+struct Pieces {
+    int cols, count, ld;      // columns of a piece (the last one's rest), pieces, row stride of the gradient
+    Pieces(int n, int V) {
+        const size_t most = PIECE_BYTES / ((size_t)n * 2) / 256 * 256;
+        const int fit = most < 256 ? 256 : most > (size_t)V ? V : (int)most;
+        count = (V + fit - 1) / fit;
+        const int even = (V + count - 1) / count;
+        cols = count == 1 ? V : (even + 255) / 256 * 256;
+        count = (V + cols - 1) / cols;
+        ld = (cols + 63) / 64 * 64;
+    }
+};
+
+int slots_of(const Plan &p, int V) { return 2 * ((V + tile_cols(p.kind) - 1) / tile_cols(p.kind)); }
+
+struct Work { size_t xs, stats, target, rows, g, dxs, sums, sums_bytes, total; };
+Work work_layout(int n, int V, int H) {
+    const Plan logits = whole_plan(0, n, V, H);
+    const Pieces pc(n, V);
+    Work w{};
+    Bump fwd;
+    w.xs = fwd.take((size_t)n * H * 2);
+    Bump bwd = fwd;
+    w.stats = fwd.take((size_t)slots_of(logits, V) * n * 8);
+    w.target = fwd.take((size_t)n * 4);
+    w.rows = bwd.take((size_t)n * sizeof(LossRow));
+    w.dxs = bwd.take((size_t)n * H * 2);
+    w.g = bwd.take((size_t)n * pc.ld * 2);
+    if (pc.count > 1) {
+        const Plan p = whole_plan(1, n, H, pc.cols);
+        w.sums_bytes = (size_t)pc.count * p.n_full * tile_rows(p.kind) * tile_cols(p.kind) * 4;
+    } else {
+        w.sums_bytes = gemm_workspace_bytes(1, n, H, V);
+    }
+    w.sums = bwd.take(w.sums_bytes);
+    w.total = fwd.off > bwd.off ? fwd.off : bwd.off;
+    return w;
+}
+
+int validate_desc(const ob_lm_loss_desc *desc, const char *who) {
+    if (!desc) return fail(OB_EINVAL, "%s: desc is null", who);
+    if (desc->dtype != OB_BF16 && desc->dtype != OB_FP32) return fail(OB_EINVAL, "%s: unknown dtype %d", who, desc->dtype);
+    if (desc->hidden < 64 || desc->vocab < 1) return fail(OB_EINVAL, "%s: non-positive dimension", who);
+    if (desc->hidden % 64) return fail(OB_EUNSUPPORTED, "%s: hidden must be a multiple of 64", who);
+    if (desc->hidden > MAX_HIDDEN) return fail(OB_EUNSUPPORTED, "%s: hidden > %d", who, MAX_HIDDEN);
+    if (desc->vocab > MAX_VOCAB) return fail(OB_EUNSUPPORTED, "%s: vocab > %d", who, MAX_VOCAB);
+    return OB_OK;
+}
+size_t bytes_of(const ob_lm_loss_desc *desc, int n) {
+    return desc->dtype == OB_FP32 ? f32::lm_loss_work_bytes(n, desc->hidden, desc->vocab) : work_layout(n, desc->vocab, desc->hidden).total;
+}
+
+bool aligned16(const void *p) { return (uintptr_t)p % 16 == 0; }
+
+int validate(const ob_lm_loss_desc *desc, const void *w, const void *x, int total_tokens, const int32_t *rows_host, const int32_t *rows_dev,
+             int n_rows, const int32_t *labels, const void *ws, size_t ws_bytes, const char *who) {
+    if (int rc = validate_desc(desc, who)) return rc;
+    if (!w || !x || !labels) return fail(OB_EINVAL, "%s: w / x / labels is null", who);
+    if (total_tokens < 1 || total_tokens > MAX_TOKENS) return fail(OB_EINVAL, "%s: total_tokens %d outside [1, %d]", who, total_tokens, MAX_TOKENS);
+    if (n_rows < 1 || n_rows > total_tokens) return fail(OB_EINVAL, "%s: n_rows %d outside [1, total_tokens]", who, n_rows);
+    if (!rows_host != !rows_dev) return fail(OB_EINVAL, "%s: rows need a host and a device copy", who);
+    if (!rows_host && n_rows != total_tokens) return fail(OB_EINVAL, "%s: without a row list n_rows is total_tokens", who);
+    if (rows_host)
+        for (int i = 0, last = -1; i < n_rows; last = rows_host[i++])
+            if (rows_host[i] <= last || rows_host[i] >= total_tokens)
+                return fail(OB_EINVAL, "%s: rows[%d] = %d, must ascend inside [0, %d)", who, i, rows_host[i], total_tokens);
+    if (!aligned16(w) || !aligned16(x)) return fail(OB_EINVAL, "%s: tensors must be aligned to 16 bytes", who);
+    if (!ws || !aligned16(ws) || ws_bytes < bytes_of(desc, n_rows))
+        return fail(OB_EWORKSPACE, "%s: workspace too small (%zu bytes given) or not aligned", who, ws_bytes);
+    return OB_OK;
+}
+
+}  // namespace
+
+extern "C" size_t ob_lm_loss_workspace_bytes(const ob_lm_loss_desc *desc, int n_rows) {
+    if (validate_desc(desc, "ob_lm_loss_workspace_bytes") || n_rows < 1 || n_rows > MAX_TOKENS) return 0;
+    return bytes_of(desc, n_rows);
+}
+
+extern "C" int ob_lm_loss_fwd(const ob_lm_loss_desc *desc, const void *w, const void *x, int total_tokens, const int32_t *rows_host,
+                              const int32_t *rows_dev, int n_rows, const int32_t *labels, float *nll, float *lse, void *ws,
+                              size_t ws_bytes, void *hip_stream) {
+    const char *who = "ob_lm_loss_fwd";
+    if (int rc = validate(desc, w, x, total_tokens, rows_host, rows_dev, n_rows, labels, ws, ws_bytes, who)) return rc;
+    if (!nll || !lse) return fail(OB_EINVAL, "%s: nll / lse is null", who);
+    hipStream_t s = (hipStream_t)hip_stream;
+    const int n = n_rows, V = desc->vocab, H = desc->hidden;
+    if (desc->dtype == OB_FP32) {
+        f32::lm_loss_fwd(w, x, rows_dev, n, H, V, labels, nll, lse, ws, s);
+        return check_launch(who);
+    }
+    const Work wk = work_layout(n, V, H);
+    unsigned char *at = (unsigned char *)ws;
+    const void *xs = x;
+    if (rows_dev) {
+        launch_rows_gather(at + wk.xs, x, rows_dev, n, H, s);
+        xs = at + wk.xs;
+    }
+    const Plan p = whole_plan(0, n, V, H);
+    launch_loss_stats(p, n, V, H, xs, w, labels, at + wk.stats, (float *)(at + wk.target), s);
+    launch_loss_combine(at + wk.stats, (const float *)(at + wk.target), labels, n, V, slots_of(p, V), nll, lse, s);
+    return check_launch(who);
+}
+
+extern "C" int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void *w, const void *x, int total_tokens,
+                              const int32_t *rows_host, const int32_t *rows_dev, int n_rows, const int32_t *labels, const float *lse,
+                              const float *dnll, void *dx, void *dw, void *ws, size_t ws_bytes, void *hip_stream) {
+    const char *who = "ob_lm_loss_bwd";
+    if (int rc = validate(desc, w, x, total_tokens, rows_host, rows_dev, n_rows, labels, ws, ws_bytes, who)) return rc;
+    if (flags & ~OB_BWD_ACCUMULATE) return fail(OB_EINVAL, "%s: unknown flag bits %d", who, flags);
+    if (!lse || !dnll || !dx || !dw) return fail(OB_EINVAL, "%s: lse / dnll / dx / dw is null", who);
+    if (!aligned16(dx) || !aligned16(dw)) return fail(OB_EINVAL, "%s: tensors must be aligned to 16 bytes", who);
+    hipStream_t s = (hipStream_t)hip_stream;
+    const int n = n_rows, V = desc->vocab, H = desc->hidden, acc = flags & OB_BWD_ACCUMULATE;
+    if (desc->dtype == OB_FP32) {
+        f32::lm_loss_bwd(w, x, total_tokens, rows_dev, n, H, V, labels, lse, dnll, dx, dw, acc ? 1 : 0, ws, s);
+        return check_launch(who);
+    }
+    const Work wk = work_layout(n, V, H);
+    const Pieces pc(n, V);
+    unsigned char *at = (unsigned char *)ws;
+    const void *xs = x;
+    void *dxs = dx;
+    if (rows_dev) {
+        launch_rows_gather(at + wk.xs, x, rows_dev, n, H, s);
+        xs = at + wk.xs;
+        dxs = at + wk.dxs;
+    }
+    LossRow *rows = (LossRow *)(at + wk.rows);
+    launch_loss_rows(lse, dnll, labels, n, V, rows, s);
+    // Per piece of the vocabulary: G = (softmax - one-hot) weight, its logits computed again; dW rows of the piece = G^T x, whole; dx += G W
+    const Plan p_dx = whole_plan(1, n, H, pc.cols);
+    float *sums = (float *)(at + wk.sums);
+    unsigned char *g = at + wk.g;
+    for (int i = 0; i < pc.count; ++i) {
+        const int v0 = i * pc.cols, cols = V - v0 < pc.cols ? V - v0 : pc.cols, ld = (cols + 63) / 64 * 64;
+        const unsigned char *wp = (const unsigned char *)w + (size_t)v0 * H * 2;
+        unsigned char *dwp = (unsigned char *)dw + (size_t)v0 * H * 2;
+        launch_loss_grad(whole_plan(0, n, cols, H), n, cols, H, xs, wp, rows, v0, g, ld, s);
+        launch_gemm_tn(cols, H, n, g, ld, xs, dwp, acc ? dwp : nullptr, s);
+        if (pc.count > 1) launch_gemm_nn_piece(p_dx, n, H, cols, g, ld, wp, sums, i, s);
+        else launch_gemm_nn(n, H, cols, g, ld, wp, dxs, wk.sums_bytes ? sums : nullptr, wk.sums_bytes, s);
+    }
+    if (pc.count > 1) launch_gemm_nn_sum(p_dx, n, H, sums, pc.count, dxs, s);
+    if (rows_dev) launch_rows_spread(dxs, dx, rows_dev, n, total_tokens, H, s);
+    return check_launch(who);
+}

@@ -1,0 +1,271 @@
+"""Cross entropy over a vocabulary: against its definition in 64 bits, and what is refused."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_20761_amd as ob
+
+gpu = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -8        # half a step of bf16
+
+
+def expected(w, xs, labels, dnll, u):
+    """{name: (value, bound)} of nll, lse, dx (of the listed rows) and dw, all in 64 bits.  A logit is off by up to 1e-5 of its terms' sum (fp32
+    sums of 64 - 4096 products; roundings that do not all go one way); G is rounded once (u) and carries the logits' error in its
+    exponential; dx and dw are rounded once and add the errors of G, and fp32 sums of theirs"""
+    w, xs, dnll = w.double(), xs.double(), dnll.double()
+    V = w.shape[0]
+    z = xs @ w.t()
+    dz = 1e-5 * (xs.abs() @ w.abs().t()).max(1).values + 1e-6
+    lse = torch.logsumexp(z, 1)
+    has = (labels >= 0) & (labels < V)
+    safe = torch.where(has, labels, 0).long()[:, None]
+    hot = torch.zeros_like(z).scatter_(1, safe, has.double()[:, None])
+    zero = torch.zeros_like(lse)
+    weight = torch.where(has, dnll, zero)[:, None]
+    P = torch.exp(z - lse[:, None])
+    G = torch.where(has[:, None], (P - hot) * weight, 0.0)
+    G_err = u * G.abs() + (2 * dz[:, None] + 1e-6 * (z.abs().max(1, keepdim=True).values + 2)) * P * weight.abs()
+    out = {"nll": (torch.where(has, lse - (z * hot).sum(1), zero), 2 * dz + 1e-6 * lse.abs()), "lse": (lse, dz + 1e-6 * lse.abs())}
+    for n, g, e, other in (("dx", G, G_err, w), ("dw", G.t(), G_err.t(), xs)):
+        v = g @ other
+        out[n] = v, u * v.abs() + (e + 1e-5 * g.abs()) @ other.abs() + 1e-30
+    return out
+
+
+class Call:
+    def __init__(self, T, H, V, rows=None, dtype=torch.bfloat16, seed=0, ignored=0.1, spread=1.0):
+        print(f"lm loss: T={T} H={H} V={V} rows={'all' if rows is None else len(rows)} {dtype}", flush=True)
+        gen = torch.Generator(device=DEV).manual_seed(seed)
+        rand = lambda *s: torch.randn(s, generator=gen, device=DEV)
+        n = T if rows is None else len(rows)
+        self.T, self.n, self.V = T, n, V
+        self.x, self.w = (spread * rand(T, H)).to(dtype), (rand(V, H) / H ** 0.5).to(dtype)
+        self.labels = torch.randint(0, V, (n,), generator=gen, device=DEV, dtype=torch.int32)
+        drop = torch.rand(n, generator=gen, device=DEV) < ignored
+        drop[0] = False
+        self.labels[drop] = torch.tensor([-100, -1, V, 2 ** 31 - 1], dtype=torch.int32, device=DEV)[torch.arange(int(drop.sum()), device=DEV) % 4]
+        self.dnll = rand(n) / n
+        self.code = ob.OB_BF16 if dtype == torch.bfloat16 else ob.OB_FP32
+        self.desc = ob.make_lm_loss_desc(H, V, self.code)
+        self.rows = None if rows is None else ob.RowIndex(rows, device=DEV)
+        nan = lambda t: torch.full_like(t, float("nan"))
+        self.nll, self.lse, self.dx, self.dw = nan(self.dnll), nan(self.dnll), nan(self.x), nan(self.w)
+        size = ob.ob_lm_loss_workspace_bytes(self.desc, n)
+        assert size > 0
+        self.ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+
+    def fwd(self, stream=None):
+        ob.ob_lm_loss_fwd(self.desc, self.w, self.x, self.T, self.rows, self.labels, self.nll, self.lse, self.ws, stream)
+
+    def bwd(self, flags=0, stream=None):
+        ob.ob_lm_loss_bwd(self.desc, flags, self.w, self.x, self.T, self.rows, self.labels, self.lse, self.dnll, self.dx, self.dw, self.ws, stream)
+
+    def run(self):
+        self.fwd()
+        self.ws.fill_(255)          # nothing in it is kept
+        self.bwd()
+        return self
+
+    def listed(self):
+        return torch.arange(self.T, device=DEV) if self.rows is None else self.rows.dev.long()
+
+    def check(self, old_dw=None):
+        want = expected(self.w, self.x[self.listed()], self.labels, self.dnll, U if self.code == ob.OB_BF16 else 0.0)
+        got = {"nll": self.nll, "lse": self.lse, "dx": self.dx[self.listed()], "dw": self.dw}
+        for n, (value, bound) in want.items():
+            if n == "dw" and old_dw is not None:
+                value = value + old_dw.double()
+                bound = bound + U * value.abs()
+            worst = float(((got[n].double() - value).abs() / bound).max())
+            assert worst <= 1, n
+        rest = torch.ones(self.T, dtype=torch.bool, device=DEV)
+        rest[self.listed()] = False
+        assert (self.dx[rest] == 0).all()
+        none = ~((self.labels >= 0) & (self.labels < self.V))
+        assert (self.nll[none] == 0).all() and (self.dx[self.listed()[none]] == 0).all()
+
+
+def _some_rows(T, n, seed=0):
+    return np.sort(np.random.default_rng(seed).permutation(T)[:n]).astype(np.int32)
+
+
+SIZES = [(1, 64, 1), (1, 64, 2), (3, 64, 63), (5, 128, 64), (64, 64, 65), (65, 192, 1009), (128, 256, 128), (129, 320, 257), (200, 64, 4099),
+         (257, 768, 2001), (300, 1024, 8190), (31, 4096, 517), (2, 8192, 130), (1000, 64, 255), (700, 128, 12289)]
+
+
+@gpu
+@pytest.mark.parametrize("T,H,V", SIZES)
+def test_every_row(T, H, V):
+    Call(T, H, V, seed=T + V).run().check()
+
+
+@gpu
+@pytest.mark.parametrize("T,n,H,V", [(1, 1, 64, 5), (70, 1, 64, 100), (300, 299, 128, 777), (1500, 321, 256, 3001), (400, 64, 640, 33333)])
+def test_some_rows(T, n, H, V):
+    Call(T, H, V, rows=_some_rows(T, n)).run().check()
+
+
+@gpu
+@pytest.mark.parametrize("T,n,H,V", [(5, 5, 64, 3), (130, 70, 128, 1009), (600, 600, 64, 40001)])
+def test_fp32(T, n, H, V):
+    Call(T, H, V, rows=None if n == T else _some_rows(T, n), dtype=torch.float32).run().check()
+
+
+@gpu
+@pytest.mark.parametrize("T,n,H,V", [(2100, 2100, 256, 16384), (5000, 2060, 128, 32003)])
+def test_large_tiles(T, n, H, V):
+    """launches that fill the chip with the largest tiles, whole and ragged"""
+    Call(T, H, V, rows=None if n == T else _some_rows(T, n)).run().check()
+
+
+@gpu
+@pytest.mark.parametrize("n,V", [(4100, 131080), (9000, 120001)])
+def test_pieces_of_the_vocabulary(n, V):
+    """the gradient of the logits is more than a piece: the last piece is ragged"""
+    assert n * V * 2 > 1 << 30
+    c = Call(n, 64, V).run()
+    c.check()
+    first = c.dx.clone(), c.dw.clone()
+    c.dx.fill_(float("nan"))
+    c.dw.fill_(float("nan"))
+    c.bwd()
+    assert torch.equal(first[0], c.dx) and torch.equal(first[1], c.dw)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H,V", [(65, 128, 1001), (300, 64, 9000)])
+def test_accumulate(T, H, V, dtype):
+    c = Call(T, H, V, dtype=dtype)
+    old = torch.randn(c.dw.shape, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).to(dtype) * 0.1
+    c.fwd()
+    c.dw.copy_(old)
+    c.bwd(ob.OB_BWD_ACCUMULATE)
+    want = expected(c.w, c.x, c.labels, c.dnll, U if dtype == torch.bfloat16 else 0.0)["dw"]
+    value = want[0] + old.double()
+    worst = float(((c.dw.double() - value).abs() / (want[1] + torch.finfo(dtype).eps / 2 * value.abs() + 1e-30)).max())
+    assert worst <= 1
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_no_row_has_a_label(dtype):
+    c = Call(70, 64, 100, dtype=dtype)
+    c.labels.fill_(-100)
+    c.run()
+    assert (c.nll == 0).all() and (c.dx == 0).all() and (c.dw == 0).all() and torch.isfinite(c.lse).all()
+
+
+@gpu
+def test_large_logits():
+    """logits of +-1000: the probabilities are 0 and 1, losses in the hundreds"""
+    c = Call(130, 64, 3000, spread=300.0).run()
+    c.check()
+    assert float(c.nll.max()) > 500
+
+
+@gpu
+def test_an_ignored_row_does_not_read_its_weight():
+    c = Call(40, 64, 90).run()
+    first = c.dx.clone(), c.dw.clone()
+    c.dnll[(c.labels < 0) | (c.labels >= c.V)] = float("nan")
+    c.bwd()
+    assert torch.equal(first[0], c.dx) and torch.equal(first[1], c.dw)
+
+
+@gpu
+def test_gradient_against_differences():
+    """fp32: the loss along a direction in x and w; 1e-3 steps leave 1e-6 of curvature and 1e-7 / 1e-3 of the loss' rounding"""
+    c = Call(50, 64, 300, dtype=torch.float32).run()
+    dx, dw = c.dx.double(), c.dw.double()
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    ux, uw = (torch.randn(t.shape, generator=gen, device=DEV) for t in (c.x, c.w))
+    h, ends, x0, w0 = 1e-3, [], c.x.clone(), c.w.clone()
+    for sign in (1, -1):
+        c.x.copy_(x0 + sign * h * ux)
+        c.w.copy_(w0 + sign * h * uw)
+        c.fwd()
+        ends.append(float((c.nll.double() * c.dnll.double()).sum()))
+    slope, exact = (ends[0] - ends[1]) / (2 * h), float((dx * ux).sum() + (dw * uw).sum())
+    size = float((dx * ux).abs().sum() + (dw * uw).abs().sum())
+    loss = float((c.nll * c.dnll).abs().sum())
+    assert abs(slope - exact) <= 1e-4 * size + 2 ** -23 * loss / h
+
+
+@gpu
+def test_side_stream_and_captured_calls():
+    c = Call(500, 128, 3001, rows=_some_rows(500, 200)).run()
+    keep = lambda: [t.clone() for t in (c.nll, c.lse, c.dx, c.dw)]
+    poison = lambda: [t.fill_(float("nan")) for t in (c.nll, c.lse, c.dx, c.dw)]
+    want = keep()
+    side = torch.cuda.Stream()
+    poison()
+    side.wait_stream(torch.cuda.current_stream())
+    c.fwd(side)
+    c.bwd(0, side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(keep(), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.fwd()
+        c.bwd()
+    for _ in range(3):
+        poison()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(keep(), want))
+        c.run()
+    # the graph reads its inputs anew
+    c.x.mul_(0.5)
+    graph.replay()
+    got = keep()
+    c.run()
+    assert all(torch.equal(a, b) for a, b in zip(keep(), got))
+
+
+# ---- refusals: no GPU ------------------------------------------------------------------------------
+
+def _i32(values):
+    return (C.c_int32 * max(len(values), 1))(*values)
+
+
+@pytest.mark.parametrize("status,text,kw", [
+    (3, "multiple of 64", {"H": 100}), (1, "dimension", {"H": 0}), (3, "hidden >", {"H": 8256}), (1, "dimension", {"V": 0}), (3, "vocab >", {"V": (1 << 21) + 1}),
+    (1, "dtype", {"dtype": 3}), (1, "null", {"w": None}), (1, "null", {"labels": None}), (1, "null", {"lse": None}),
+    (1, "total_tokens", {"T": 0}), (1, "total_tokens", {"T": (1 << 22) + 1}), (1, "n_rows", {"n": 0}), (1, "n_rows", {"n": 11}),
+    (1, "host and a device", {"rows_dev": None}), (1, "rows[1] = 1", {"rows": (1, 1, 2)}), (1, "rows[2] = 10", {"rows": (1, 2, 10)}),
+    (1, "rows[0] = -1", {"rows": (-1, 2, 3)}), (1, "rows[1] = 3", {"rows": (4, 3, 5)}), (1, "without a row list", {"rows": None, "rows_dev": None}),
+    (1, "aligned", {"x": 0x1004}), (4, "workspace", {"ws": None}), (4, "workspace", {"ws_bytes": 16}), (4, "workspace", {"ws": 0x1008}),
+])
+def test_refusals(status, text, kw):
+    a = dict(H=128, V=1000, dtype=0, w=0x1000, x=0x1000, T=10, rows=(1, 4, 7), rows_dev=0x1000, n=3, labels=0x1000, nll=0x1000, lse=0x1000,
+             dnll=0x1000, dx=0x1000, dw=0x1000, ws=0x1000, ws_bytes=1 << 40, flags=0)
+    a.update(kw)
+    desc = ob.make_lm_loss_desc(a["H"], a["V"], a["dtype"])
+    p = lambda n: C.c_void_p(a[n])
+    rows = None if a["rows"] is None else _i32(a["rows"])
+    front = (p("w"), p("x"), a["T"], rows, p("rows_dev"), a["n"], p("labels"))
+    st = ob.lib.ob_lm_loss_fwd(C.byref(desc), *front, p("nll"), p("lse"), p("ws"), a["ws_bytes"], None)
+    assert st == status and text in ob.ob_last_error(), ob.ob_last_error()
+    st = ob.lib.ob_lm_loss_bwd(C.byref(desc), a["flags"], *front, p("lse"), p("dnll"), p("dx"), p("dw"), p("ws"), a["ws_bytes"], None)
+    assert st == status and text in ob.ob_last_error(), ob.ob_last_error()
+
+
+def test_refusals_of_the_backward():
+    desc, p = ob.make_lm_loss_desc(128, 1000), C.c_void_p(0x1000)
+    for flags, dx, text in ((ob.OB_BWD_RECOMPUTE, p, "flag"), (8, p, "flag"), (0, None, "null"), (0, C.c_void_p(0x1002), "aligned")):
+        st = ob.lib.ob_lm_loss_bwd(C.byref(desc), flags, p, p, 3, None, None, 3, p, p, p, dx, p, p, 1 << 40, None)
+        assert st == ob.OB_EINVAL and text in ob.ob_last_error()
+
+
+def test_workspace_bytes():
+    size = lambda H, V, n, dtype=0: ob.ob_lm_loss_workspace_bytes(ob.make_lm_loss_desc(H, V, dtype), n)
+    assert size(100, 10, 1) == 0 and size(64, 10, 0) == 0 and size(64, 10, (1 << 22) + 1) == 0
+    # the gradient of the logits is kept within a piece: twice the vocabulary takes no second GiB, but for dx's sums and the maxima
+    a, b = size(4096, 131072, 8192), size(4096, 262144, 8192)
+    assert 2 << 29 < a < b < a + (1 << 30)
+    assert size(64, 1000, 100, 1) >= 100 * 1000 * 4
