@@ -353,11 +353,10 @@ struct Sinks { static constexpr bool BAND = false, SINKS = true; int window, sin
 // of the segment in front of the band are left out.
 template <class WIN>
 struct BandTiles {
-    static constexpr int skip = 0, n_head = 0, sink_end = 0;
+    static constexpr int skip = 0, n_head = 0, window = 0, sink_end = 0;
     __device__ __forceinline__ BandTiles(const TileInfo &, const WIN &, int) {}
     __device__ __forceinline__ int row(int j) const { return j * ST; }       // first key row of tile j, from the segment's start
-    __device__ __forceinline__ int from(int) const { return 0; }             // first key of a row's band
-    __device__ __forceinline__ bool wave_sees(int, int) const { return true; }
+    __device__ __forceinline__ bool wave_sees(int, int) const { return true; }      // some row of the wave, keys of the band in these
 };
 template <>
 struct BandTiles<Band> {
@@ -375,8 +374,7 @@ struct BandTiles<Band> {
         n_head = min(whole, (last + ST) / ST) - skip;
     }
     __device__ __forceinline__ int row(int j) const { return (apart && j == 0 ? 0 : j + skip) * ST; }
-    __device__ __forceinline__ int from(int q_row) const { return q_row - window + 1; }
-    __device__ __forceinline__ bool wave_sees(int kv_first, int rows) const { return kv_first + rows > wave_from || kv_first < sink_end; }
+    __device__ __forceinline__ bool wave_sees(int kv_first, int rows) const { return kv_first + rows > wave_from; }
 };
 
 // LDS reads are issued one batch ahead of the MFMAs that consume them (explicit double buffers and
@@ -389,12 +387,13 @@ struct BandTiles<Band> {
         __builtin_amdgcn_sched_barrier(0);                         \
     } while (0)
 
-// BAND: keys in front of `from` are seen below `sink_end` alone.
-template <int D, bool CAUSAL, bool MASK, bool BAND = false>
+// BAND: a row sees its last `window` keys; SINK: and the tile's keys below sink_end.  As an unsigned number the distance from key to row is below the
+// window for just the keys of the band, those behind the row and past the segment's end left out: one comparison.
+template <int D, bool CAUSAL, bool MASK, bool BAND = false, bool SINK = false>
 __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict__ ks,
                                          const unsigned char OB_LDS *__restrict__ vs, const Tile<D> &tl,
                                          const bf16x8 (&qf)[D / 16], f32x16 (&acc_o)[D / 32], float &m_run,
-                                         float &l_run, int kv0, int seg_end, int q_row, float sl2, int from = 0, int sink_end = 0) {
+                                         float &l_run, int kv0, int seg_end, int q_row, float sl2, int window = 0, int sink_end = 0) {
     const int lh = (threadIdx.x & 63) >> 5;
     constexpr int HB = 2;                 // K fragments (D-steps) per batch
     constexpr int R = D == 128 ? 3 : 2;   // batches in flight (ring depth)
@@ -431,13 +430,15 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
     }
     // the running maximum is kept on the raw scores; the softmax scale rides in the exponent's FMA
     float mx = NEG_BIG;
+    const int dist = q_row - kv0 - 4 * lh, below = min(sink_end - kv0 - 4 * lh, dist + 1);
     if (MASK) {
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int kv = kv0 + mt * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
-                const bool ok = kv < seg_end && (!CAUSAL || kv <= q_row) && (!BAND || kv >= from || kv < sink_end);
+                const int c = mt * 32 + 8 * (r >> 2) + (r & 3);
+                const bool ok = BAND ? (unsigned)(dist - c) < (unsigned)window || (SINK && c < below) : kv < seg_end && (!CAUSAL || kv <= q_row);
                 const float s = ok ? acc_s[mt][r] : NEG_BIG;
                 acc_s[mt][r] = s;
                 mx = fmaxf(mx, s);
@@ -576,9 +577,15 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
         if (!(MASKED))                                                                                   \
             fwd_tile<D, CAUSAL, false>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0, ti.seg_end, q_row,  \
                                        sl2);                                                             \
-        else if (!(CAUSAL && kv0 > wave_q_last) && bt.wave_sees(kv0, ST))                                \
-            fwd_tile<D, CAUSAL, true, WIN::BAND>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0,           \
-                                                 ti.seg_end, q_row, sl2, bt.from(q_row), bt.sink_end);   \
+        else if (!(CAUSAL && kv0 > wave_q_last)) {                                                       \
+            if (WIN::BAND && kv0 < bt.sink_end)                                                          \
+                fwd_tile<D, CAUSAL, true, WIN::BAND, WIN::BAND>((KS), (VS), tl, qf, acc_o, m_run, l_run, \
+                                                                kv0, ti.seg_end, q_row, sl2, bt.window,  \
+                                                                bt.sink_end);                            \
+            else if (bt.wave_sees(kv0, ST))                                                              \
+                fwd_tile<D, CAUSAL, true, WIN::BAND>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0,       \
+                                                     ti.seg_end, q_row, sl2, bt.window);                 \
+        }                                                                                                \
         ++j;                                                                                             \
     }
 #define OB_FWD_ANY(MASKED) OB_FWD_ITER(MASKED, (j & 1) ? ks1 : ks0, (j & 1) ? vs1 : vs0, (j & 1) ? ks0 : ks1, (j & 1) ? vs0 : vs1)
@@ -624,12 +631,12 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
 // on one half of the tile with their partial dQ added at the end, asked the L2 for twice the bytes
 // per MFMA (4.7 GB per launch on the 7B-shaped batch, 10 TB/s) and had a barrier per 24 MFMAs.
 // ------------------------------------------------------------------------------------------------
-template <int D, bool CAUSAL, bool MASK, bool BAND = false>
+template <int D, bool CAUSAL, bool MASK, bool BAND = false, bool SINK = false>
 __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__ ks,
                                         const unsigned char OB_LDS *__restrict__ vs, const Tile<D> &tl,
                                         const bf16x8 (&qf)[D / 16], const bf16x8 (&dof)[D / 16],
                                         f32x16 (&acc_dq)[D / 32], float lse2, float dlt, int kv_first,
-                                        int seg_end, int q_row, float sl2, int from = 0, int sink_end = 0) {
+                                        int seg_end, int q_row, float sl2, int window = 0, int sink_end = 0) {
     // ks / vs point at a 32-row half of the K / V tile; kv_first is its first key row
     const int lh = (threadIdx.x & 63) >> 5;
     constexpr int HB = 2;             // D-steps per batch (a batch reads HB fragments of K and HB of V)
@@ -666,6 +673,7 @@ __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__
     }
     // dS of contraction step h (8 values per lane, rounded to bf16); step 1's are worked out between the
     // MFMAs of step 0, so the wave's own element-wise work runs in the shadow of its matrix instructions
+    const int dist = q_row - kv_first - 4 * lh, below = min(sink_end - kv_first - 4 * lh, dist + 1);
     auto dscores = [&](int h) {
         bf16x8 o;
 #pragma unroll
@@ -674,7 +682,8 @@ __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__
             bool ok = true;
             if (MASK) {
                 const int kv = kv_first + 8 * (r >> 2) + 4 * lh + (r & 3);
-                ok = kv < seg_end && (!CAUSAL || kv <= q_row) && (!BAND || kv >= from || kv < sink_end);
+                const int c = 8 * (r >> 2) + (r & 3);
+                ok = BAND ? (unsigned)(dist - c) < (unsigned)window || (SINK && c < below) : kv < seg_end && (!CAUSAL || kv <= q_row);
             }
             const float p = ok ? fast_exp2(acc_s[r] * sl2 - lse2) : 0.f;
             o[e] = (__bf16)(p * (acc_dp[r] - dlt));
@@ -789,11 +798,16 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
                 if (wave_live)                                                                               \
                     dq_half<D, CAUSAL, false>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, acc_dq, lse2,  \
                                               dlt, kv_first, ti.seg_end, q_row, sl2);                        \
-            } else if (wave_live && kv_first < ti.seg_end && !(CAUSAL && kv_first > wave_q_last) &&          \
-                       bt.wave_sees(kv_first, 32))                                                           \
-                dq_half<D, CAUSAL, true, WIN::BAND>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, acc_dq,  \
-                                                    lse2, dlt, kv_first, ti.seg_end, q_row, sl2,             \
-                                                    bt.from(q_row), bt.sink_end);                            \
+            } else if (wave_live && kv_first < ti.seg_end && !(CAUSAL && kv_first > wave_q_last)) {          \
+                if (WIN::BAND && kv_first < bt.sink_end)                                                     \
+                    dq_half<D, CAUSAL, true, WIN::BAND, WIN::BAND>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, \
+                                                                   acc_dq, lse2, dlt, kv_first, ti.seg_end,  \
+                                                                   q_row, sl2, bt.window, bt.sink_end);      \
+                else if (bt.wave_sees(kv_first, 32))                                                         \
+                    dq_half<D, CAUSAL, true, WIN::BAND>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof,     \
+                                                        acc_dq, lse2, dlt, kv_first, ti.seg_end, q_row, sl2, \
+                                                        bt.window);                                          \
+            }                                                                                                \
         }                                                                                                    \
         ++j;                                                                                                 \
     }
@@ -869,10 +883,10 @@ __device__ __forceinline__ void dkv_scores(const unsigned char OB_LDS *__restric
 
 // role P: probabilities of the 32 MT x 32 score tile, packed as the second operands of the 2 MT
 // 16-row contraction steps (pk[mt][h] serves step 2 mt + h)
-// (BAND: rows `window` and more behind the key do not see it)
-template <bool CAUSAL, bool MASK, int MT, bool BAND = false>
+// (SPAN: the rows that see the key are the `span` from its own on)
+template <bool CAUSAL, bool MASK, int MT, bool SPAN = false>
 __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned char OB_LDS *__restrict__ lse2_s,
-                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2], int window = 0) {
+                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2], int span = 0) {
     const int lh = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -885,7 +899,7 @@ __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned 
                 bool ok = true;
                 if (MASK) {
                     const int qr = q0 + mt * 32 + 8 * g + 4 * lh + e;
-                    ok = qr < seg_end && (!CAUSAL || kv_row <= qr) && (!BAND || qr - kv_row < window);
+                    ok = SPAN ? (unsigned)(qr - kv_row) < (unsigned)span : qr < seg_end && (!CAUSAL || kv_row <= qr);
                 }
                 const float pe = fast_exp2(s[mt][4 * g + e] * sl2 - l4[e]);
                 p[4 * g + e] = ok ? pe : 0.f;
@@ -1197,6 +1211,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
     const int kv_row = min(ti.row0 + pair * 32 + lx, ti.seg_end - 1);
     const bool kv_live = ti.row0 + pair * 32 + lx < ti.seg_end;
     const int pair_kv_first = ti.row0 + pair * 32;
+    const int span = min(q_end - kv_row, WIN::BAND ? window : MAX_TOKENS);
     auto band_is_past = [&](int q0) __attribute__((always_inline)) { return q0 - (pair_kv_first + 31) >= window; };
     const float sl2 = scale * LOG2E;
     constexpr int KT = D / 16, DT = D / 32;
@@ -1288,7 +1303,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
                 for (int i = 0; i < 2 * MT; ++i) pk[i >> 1][i & 1] = pn[i >> 1][i & 1];
             } else {
                 if (FUSE && late) dkv_outputs<D, MT>(tiles + PREV * BYTES, tl, pk, acc_out);
-                if (live) dkv_probs<CAUSAL, MASK, MT, WIN::BAND>(acc_x, stat + S * 256, q0, q_end, kv_row, sl2, pk, window);
+                if (live) dkv_probs<CAUSAL, MASK, MT, WIN::BAND || WIN::SINKS>(acc_x, stat + S * 256, q0, ti.seg_end, kv_row, sl2, pk, span);
             }
             if (live) {
 #pragma unroll
@@ -1590,21 +1605,31 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
 }
 
 // dK and dV of the sinks of every segment longer than the window: the fp32 sums of its chunks, in order, then one rounding.  Workgroups
-// (place, key/value head, 1024 elements), those of a segment's first chunk at work.
+// (place, key/value head, 256 elements), those of a segment's first chunk at work; a wave adds a quarter of the chunks.
 template <int D>
 __global__ __launch_bounds__(256) void attn_sink_sum_kernel(const float *__restrict__ part, __bf16 *__restrict__ dk, __bf16 *__restrict__ dv,
                                                             int ldkv, const int32_t *__restrict__ cu, int n_seg, Sinks win, float scale) {
     __shared__ int sh[8];
+    __shared__ f32x4 quarter[4][64];
     const int place = blockIdx.x, kvh = blockIdx.y, nkv = gridDim.y;
     const TileInfo ti = find_tile<true>(cu, n_seg, win.chunk, sh, place, win.window);
     if (ti.row0 != ti.seg_start) return;
     const int len = ti.seg_end - ti.seg_start, chunks = (len + win.chunk - 1) / win.chunk;
-    const int e = (blockIdx.z * 256 + threadIdx.x) * 4, role = e / (win.sinks * D), r = e - role * win.sinks * D;
-    if (role > 1 || r / D >= len) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (blockIdx.z * 64 + lane) * 4;
+    const int role = e / (win.sinks * D), r = e - role * win.sinks * D;
+    const bool live = role < 2 && r / D < len;
     const size_t slot = (size_t)nkv * 2 * win.sinks * D;
     const float *src = part + (size_t)place * slot + (size_t)kvh * 2 * win.sinks * D + e;
-    f32x4 sum = *(const f32x4 *)src;
-    for (int c = 1; c < chunks; ++c) sum += *(const f32x4 *)(src + c * slot);
+    const int per = (chunks + 3) / 4, end = min(chunks, (wave + 1) * per);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (live) {
+#pragma unroll 8
+        for (int c = wave * per; c < end; ++c) sum += *(const f32x4 *)(src + c * slot);
+    }
+    quarter[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || !live) return;
+    sum = quarter[0][lane] + quarter[1][lane] + quarter[2][lane] + quarter[3][lane];
     const float f = role ? scale : 1.f;
     bf16x4 out;
 #pragma unroll
@@ -1804,10 +1829,10 @@ void launch_attn_window_bwd(const void *d_o, const void *q, const void *k, const
     const Band band{window, sinks};
     if (d == 64) hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, window_np(64), window_sr(64), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
     else hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, window_np(128), window_sr(128), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
-    const int chunks = sink_chunks(seg, window, sinks);
+    const int chunks = sink_chunks(seg, d, window, sinks);
     if (!chunks) return;
-    const Sinks first{window, sinks, sink_chunk_rows(window), part};
-    const dim3 grid_s((unsigned)chunks * nkv), grid_r(chunks, nkv, (2 * sinks * d + 1023) / 1024);
+    const Sinks first{window, sinks, sink_chunk_rows(d), part};
+    const dim3 grid_s((unsigned)chunks * nkv), grid_r(chunks, nkv, (2 * sinks * d + 255) / 256);
     ord.n = 0;
     if (d == 64) {
         hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, 2, window_sr(64), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));

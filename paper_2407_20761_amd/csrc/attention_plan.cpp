@@ -56,10 +56,9 @@ int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side,
     return n << log2;
 }
 
-int sink_chunk_rows(int window) { return std::min(2048, std::max(256, (window + 64 + ST - 1) / ST * ST)); }
-int sink_chunks(const ob_segments *seg, int window, int sinks) {
+int sink_chunks(const ob_segments *seg, int d, int window, int sinks) {
     if (!sinks) return 0;
-    const int rows = sink_chunk_rows(window);
+    const int rows = sink_chunk_rows(d);
     int n = 0;
     for (int j = 0; j < seg->n_seg; ++j) {
         const int len = seg->cu_host[j + 1] - seg->cu_host[j];

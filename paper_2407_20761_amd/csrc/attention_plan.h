@@ -55,9 +55,9 @@ int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal);
 // Windowed attention: dK / dV in pairs of 32 key rows and query tiles, as above
 constexpr int window_np(int d) { return d == 64 ? 2 : 4; }
 constexpr int window_sr(int d) { return d == 64 ? 32 : 64; }
-// Rows of a chunk of queries that the sinks' sums are split into: about what a workgroup of the windowed launch walks, in whole tiles, and how
-// many such chunks the segments longer than the window have
-int sink_chunk_rows(int window);
-int sink_chunks(const ob_segments *seg, int window, int sinks);
+// Rows of a chunk of queries that the sinks' sums are split into (of its own: not of the batch, so that a segment gives the same sums in every batch), and
+// how many such chunks the segments longer than the window have
+constexpr int sink_chunk_rows(int d) { return d == 64 ? 256 : 256; }
+int sink_chunks(const ob_segments *seg, int d, int window, int sinks);
 
 }  // namespace ob

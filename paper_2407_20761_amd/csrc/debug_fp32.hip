@@ -291,6 +291,8 @@ __global__ __launch_bounds__(256) void attn_bwd_dq_kernel(const float *__restric
 }
 
 // dk[j, kvh] = scale sum_{heads of the group} sum_t dS_tj q_t;  dv[j, kvh] = sum sum P_tj dO_t
+// SHARED waves to a key row, each every SHARED-th of its queries (with sinks, a key that all of a long segment sees would keep the launch waiting)
+template <int SHARED>
 __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(const float *__restrict__ d_o, const float *__restrict__ q,
                                                            const float *__restrict__ k, const float *__restrict__ v,
                                                            const float *__restrict__ lse, const float *__restrict__ delta,
@@ -298,8 +300,10 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(const float *__restri
                                                            int ldkv, int ldo, const int32_t *__restrict__ cu, int n_seg,
                                                            int T, int nkv, int group, int d, float scale, int causal,
                                                            int window, int sinks) {
-    const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 6;
-    const int lane = threadIdx.x & 63;
+    static_assert(SHARED == 1 || SHARED == 4, "a workgroup's four waves");
+    __shared__ float sums[SHARED == 4 ? 4 : 1][4][64];
+    const long w = SHARED == 4 ? (long)blockIdx.x : ((long)blockIdx.x * 256 + threadIdx.x) >> 6;
+    const int lane = threadIdx.x & 63, mine = SHARED == 4 ? threadIdx.x >> 6 : 0;
     if (w >= (long)T * nkv) return;
     const int j = (int)(w / nkv), kvh = (int)(w % nkv);
     const int sj = segment_of(cu, n_seg, j);
@@ -311,7 +315,7 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(const float *__restri
         vv[e] = v[(size_t)j * ldkv + kvh * d + lane + 64 * e];
     }
     for (int head = kvh * group; head < (kvh + 1) * group; ++head)
-        for (int t = lo; t < hi; ++t) {
+        for (int t = lo + mine; t < hi; t += SHARED) {
             float ps = 0.f, pd = 0.f, qe[2] = {0.f, 0.f}, de[2] = {0.f, 0.f};
             for (int e = 0; e < per; ++e) {
                 qe[e] = q[(size_t)t * ldq + head * d + lane + 64 * e];
@@ -323,6 +327,13 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(const float *__restri
             const float ds = p * (wave_sum(pd) - delta[(size_t)head * T + t]);
             for (int e = 0; e < per; ++e) { av[e] += p * de[e]; ak[e] += ds * qe[e]; }
         }
+    if (SHARED == 4) {
+        for (int e = 0; e < 2; ++e) { sums[mine][e][lane] = ak[e]; sums[mine][2 + e][lane] = av[e]; }
+        __syncthreads();
+        if (mine != 0) return;
+        for (int m = 1; m < 4; ++m)
+            for (int e = 0; e < 2; ++e) { ak[e] += sums[m][e][lane]; av[e] += sums[m][2 + e][lane]; }
+    }
     for (int e = 0; e < per; ++e) {
         dk[(size_t)j * ldkv + kvh * d + lane + 64 * e] = ak[e] * scale;
         dv[(size_t)j * ldkv + kvh * d + lane + 64 * e] = av[e];
@@ -401,9 +412,11 @@ static void run_attn_bwd(const void *d_o, const void *q, const void *k, const vo
     hipLaunchKernelGGL(attn_bwd_dq_kernel, dim3(blocks_for((long)T * nq * 64)), dim3(256), 0, s, (const float *)d_o,
                        (const float *)q, (const float *)k, (const float *)v, lse, delta, (float *)dq, ldq, ldkv, ldo,
                        seg->cu_dev, seg->n_seg, T, nq, nq / nkv, d, scale, causal, window, sinks);
-    hipLaunchKernelGGL(attn_bwd_dkv_kernel, dim3(blocks_for((long)T * nkv * 64)), dim3(256), 0, s, (const float *)d_o,
-                       (const float *)q, (const float *)k, (const float *)v, lse, delta, (float *)dk, (float *)dv, ldq,
-                       ldkv, ldo, seg->cu_dev, seg->n_seg, T, nkv, nq / nkv, d, scale, causal, window, sinks);
+#define OB_ARGS (const float *)d_o, (const float *)q, (const float *)k, (const float *)v, lse, delta, (float *)dk, (float *)dv, ldq, ldkv, ldo, \
+                seg->cu_dev, seg->n_seg, T, nkv, nq / nkv, d, scale, causal, window, sinks
+    if (window < NO_WINDOW) hipLaunchKernelGGL((attn_bwd_dkv_kernel<4>), dim3((unsigned)((long)T * nkv)), dim3(256), 0, s, OB_ARGS);
+    else hipLaunchKernelGGL((attn_bwd_dkv_kernel<1>), dim3(blocks_for((long)T * nkv * 64)), dim3(256), 0, s, OB_ARGS);
+#undef OB_ARGS
 }
 
 void attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
@@ -605,6 +618,65 @@ void connector_bwd(const ob_connector_weights *w, const ob_connector_grads *gr, 
 }
 
 // ---- cross entropy over a vocabulary, fp32: logits of a few rows at a time -----------------------
+// C[m][n] (+)= sum_k A(m, k) B(n, k) as in gemm_kernel, on the fp32 matrix instruction: a workgroup to a 32 x 32 tile, its four waves a quarter of
+// the contraction each, straight from memory (a lane holds k 4 (lane / 32) .. + 3 of each 8: the same order on both sides is all that matters), their
+// sums added in order.  AK, BK: k is the operand's inner index.  (120 x 256 over K = 1009: 165 us in gemm_kernel, whose 8 tiles walk K alone.)
+template <bool AK, bool BK>
+__global__ __launch_bounds__(256) void loss_gemm_kernel(int M, int N, int K, const float *__restrict__ A, long lda, const float *__restrict__ B,
+                                                        long ldb, float *__restrict__ C, int accumulate) {
+    typedef __attribute__((ext_vector_type(4))) float f32x4;
+    typedef __attribute__((ext_vector_type(16))) float f32x16;
+    __shared__ float sums[4][32][33];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 31, h = lane >> 5;
+    const int tiles_m = (M + 31) / 32, m0 = blockIdx.x % tiles_m * 32, n0 = blockIdx.x / tiles_m * 32;
+    const long m = min(m0 + x, M - 1), n = min(n0 + x, N - 1);
+    auto load = [](const float *p, long row, long ld, int k, bool inner) {
+        f32x4 v;
+        if (inner) __builtin_memcpy(&v, p + row * ld + k, 16);
+        else
+            for (int e = 0; e < 4; ++e) v[e] = p[(long)(k + e) * ld + row];
+        return v;
+    };
+    f32x16 acc;
+    for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+    const int per = (K / 8 + 3) / 4 * 8, k_end = min(K / 8 * 8, (wave + 1) * per);
+    int k = wave * per;
+    for (; k + 32 <= k_end; k += 32) {     // four steps' loads in flight
+        f32x4 a[4], b[4];
+        for (int i = 0; i < 4; ++i) {
+            a[i] = load(A, m, lda, k + 8 * i + 4 * h, AK);
+            b[i] = load(B, n, ldb, k + 8 * i + 4 * h, BK);
+        }
+        for (int i = 0; i < 4; ++i)
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i][e], b[i][e], acc, 0, 0, 0);
+    }
+    for (; k < k_end; k += 8) {
+        const f32x4 a = load(A, m, lda, k + 4 * h, AK), b = load(B, n, ldb, k + 4 * h, BK);
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], acc, 0, 0, 0);
+    }
+    if (wave == 3)                         // the rest of K, an element at a time
+        for (k = K / 8 * 8; k < K; k += 2) {
+            const bool in = k + h < K;
+            const float a = in ? AK ? A[m * lda + k + h] : A[(k + h) * lda + m] : 0.f, b = in ? BK ? B[n * ldb + k + h] : B[(k + h) * ldb + n] : 0.f;
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, acc, 0, 0, 0);
+        }
+    for (int r = 0; r < 16; ++r) sums[wave][8 * (r >> 2) + 4 * h + (r & 3)][x] = acc[r];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 1024; i += 256) {
+        const int r = i >> 5, c = i & 31;
+        if (m0 + r >= M || n0 + c >= N) continue;
+        float *const dst = C + (size_t)(m0 + r) * N + n0 + c;
+        const float sum = sums[0][r][c] + sums[1][r][c] + sums[2][r][c] + sums[3][r][c];
+        *dst = accumulate ? *dst + sum : sum;
+    }
+}
+static void loss_gemm(int layout, int M, int N, int K, const float *A, const float *B, float *C, int accumulate, hipStream_t s) {
+    const dim3 grid((unsigned)((M + 31) / 32) * ((N + 31) / 32));
+    if (layout == 0) hipLaunchKernelGGL((loss_gemm_kernel<true, true>), grid, dim3(256), 0, s, M, N, K, A, K, B, K, C, accumulate);
+    else if (layout == 1) hipLaunchKernelGGL((loss_gemm_kernel<true, false>), grid, dim3(256), 0, s, M, N, K, A, K, B, N, C, accumulate);
+    else hipLaunchKernelGGL((loss_gemm_kernel<false, false>), grid, dim3(256), 0, s, M, N, K, A, M, B, N, C, accumulate);
+}
+
 // one workgroup to a row of z [n, V]; GRAD: z becomes (softmax - one-hot) weight
 template <bool GRAD>
 __global__ __launch_bounds__(256) void loss_row_kernel(float *__restrict__ z, int V, const int32_t *__restrict__ labels, float *__restrict__ nll,
@@ -670,7 +742,7 @@ void lm_loss_fwd(const void *w, const void *x, const int32_t *rows_dev, int n, i
     float *z = OB_FM((unsigned char *)ws + wk.z);
     for (int i = 0; i < n; i += wk.rows) {
         const int m = n - i < wk.rows ? n - i : wk.rows;
-        gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, nullptr, nullptr, 0, s);
+        loss_gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, 0, s);
         hipLaunchKernelGGL((loss_row_kernel<false>), dim3(m), dim3(256), 0, s, z, V, labels + i, nll + i, lse + i, (const float *)nullptr);
     }
 }
@@ -683,11 +755,11 @@ void lm_loss_bwd(const void *w, const void *x, int T, const int32_t *rows_dev, i
     float *z = OB_FM(wb + wk.z), *dxs = rows_dev ? OB_FM(wb + wk.dxs) : OB_FM(dx);
     for (int i = 0; i < n; i += wk.rows) {
         const int m = n - i < wk.rows ? n - i : wk.rows;
-        gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, nullptr, nullptr, 0, s);
+        loss_gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, 0, s);
         hipLaunchKernelGGL((loss_row_kernel<true>), dim3(m), dim3(256), 0, s, z, V, labels + i, (float *)nullptr, (float *)lse + i /* read only */,
                            dnll + i);
-        gemm(2, V, H, m, z, xs + (size_t)i * H, OB_FM(dw), nullptr, nullptr, accumulate || i > 0 ? 1 : 0, s);
-        gemm(1, m, H, V, z, OB_F(w), dxs + (size_t)i * H, nullptr, nullptr, 0, s);
+        loss_gemm(2, V, H, m, z, xs + (size_t)i * H, OB_FM(dw), accumulate || i > 0 ? 1 : 0, s);
+        loss_gemm(1, m, H, V, z, OB_F(w), dxs + (size_t)i * H, 0, s);
     }
     if (rows_dev) hipLaunchKernelGGL(rows_spread_kernel, dim3(T), dim3(256), 0, s, dxs, OB_FM(dx), rows_dev, n, H);
 }

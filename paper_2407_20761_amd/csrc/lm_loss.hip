@@ -21,24 +21,40 @@ __device__ __forceinline__ void join(float &m, float &sum, float m2, float sum2)
     m = top;
 }
 
-// 16 rows to a workgroup, 16 threads to a row, each every sixteenth part; stats [slots][n], so the rows of a part are read together
+// ROWS rows to a workgroup, 256 / ROWS threads to a row, each every (256 / ROWS)-th part, eight of them in flight; stats [slots][n], so the rows of a
+// part are read together
+template <int ROWS>
 __global__ __launch_bounds__(256) void loss_combine_kernel(const float2 *__restrict__ stats, const float *__restrict__ target,
                                                            const int32_t *__restrict__ labels, int n, int V, int slots,
                                                            float *__restrict__ nll, float *__restrict__ lse) {
-    __shared__ float2 sh[16][17];
-    const int row = blockIdx.x * 16 + (threadIdx.x & 15), lane = threadIdx.x >> 4;
+    constexpr int PER = 256 / ROWS, AHEAD = 8;
+    __shared__ float2 sh[PER][ROWS + 1];
+    const int r = threadIdx.x % ROWS, row = blockIdx.x * ROWS + r, lane = threadIdx.x / ROWS;
     float m = -INFINITY, sum = 0.f;
     if (row < n) {
-#pragma unroll 4
-        for (int i = lane; i < slots; i += 16) {
-            const float2 p = stats[(size_t)i * n + row];
-            join(m, sum, p.x, p.y);
+        for (int i = lane; i < slots; i += PER * AHEAD) {
+            float2 p[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int at = i + a * PER;
+                p[a] = stats[(size_t)min(at, slots - 1) * n + row];
+                if (at >= slots) p[a].y = 0.f;
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) join(m, sum, p[a].x, p[a].y);
         }
     }
-    sh[lane][threadIdx.x & 15] = float2{m, sum};
-    __syncthreads();
+    sh[lane][r] = float2{m, sum};
+    // pairs of threads, of pairs, ...: always the same order
+#pragma unroll
+    for (int half = PER / 2; half >= 1; half /= 2) {
+        __syncthreads();
+        if (lane < half) {
+            join(m, sum, sh[lane + half][r].x, sh[lane + half][r].y);
+            sh[lane][r] = float2{m, sum};
+        }
+    }
     if (lane != 0 || row >= n) return;
-    for (int i = 1; i < 16; ++i) join(m, sum, sh[i][threadIdx.x].x, sh[i][threadIdx.x].y);
     const float l = m + logf(sum);
     const int label = labels[row];
     lse[row] = l;
@@ -76,7 +92,11 @@ __global__ __launch_bounds__(256) void rows_spread_kernel(const __bf16 *__restri
 void launch_loss_combine(const void *stats, const float *target, const int32_t *labels, int n, int V, int slots, float *nll, float *lse,
                          hipStream_t s) {
     ProfScope prof(K_REDUCE, s, 8.0 * n * slots);
-    hipLaunchKernelGGL(loss_combine_kernel, dim3((n + 15) / 16), dim3(256), 0, s, (const float2 *)stats, target, labels, n, V, slots, nll, lse);
+    // few rows: more threads to each
+    if (n <= 2048)
+        hipLaunchKernelGGL((loss_combine_kernel<4>), dim3((n + 3) / 4), dim3(256), 0, s, (const float2 *)stats, target, labels, n, V, slots, nll, lse);
+    else
+        hipLaunchKernelGGL((loss_combine_kernel<16>), dim3((n + 15) / 16), dim3(256), 0, s, (const float2 *)stats, target, labels, n, V, slots, nll, lse);
 }
 void launch_loss_rows(const float *lse, const float *dnll, const int32_t *labels, int n, int V, LossRow *rows, hipStream_t s) {
     ProfScope prof(K_ROWS, s, 28.0 * n);

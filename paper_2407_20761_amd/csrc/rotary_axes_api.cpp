@@ -12,21 +12,30 @@ int rotary_table(const ob_rotary_axes_desc *desc, RotaryTable &table, const char
         return fail(OB_EINVAL, "%s: n_axes %d outside [1, %d]", who, desc->n_axes, OB_ROTARY_MAX_AXES);
     if (!(desc->base > 1.f) || !std::isfinite(desc->base)) return fail(OB_EINVAL, "%s: base must be a number > 1", who);
     const int half = desc->head_dim / 2;
-    int pairs[OB_ROTARY_MAX_AXES] = {}, seen[OB_ROTARY_MAX_AXES] = {};
+    int pairs[OB_ROTARY_MAX_AXES] = {};
     for (int i = 0; i < half; ++i) {
         const int a = desc->axis_of_pair[i];
         if (a < -1 || a >= desc->n_axes) return fail(OB_EINVAL, "%s: pair %d has axis %d, must be -1 or below n_axes %d", who, i, a, desc->n_axes);
         if (a >= 0) ++pairs[a];
     }
-    for (int i = 0; i < half; ++i) {
+    // theta / 2 pi in units of 2^-64 of a turn (theta <= 1: at most 0.16 of the range), in the 64 bits of a long double's mantissa.  A spectrum is
+    // a geometric sequence: one power, then products (64 of them, 2^-58 of the value: 2e-9 rad at the largest position; a power for each took
+    // 13 us of a call, whose launch takes 4).
+    const long double turn = ldexpl(0.159154943091895335768883763372514362L, 64), log_base = logl((long double)desc->base);
+    const auto ratio_of = [&](int n) { return expl(-log_base / n); };
+    long double theta[OB_ROTARY_MAX_AXES], ratio[OB_ROTARY_MAX_AXES], all = turn;
+    const long double ratio_all = ratio_of(half);
+    for (int a = 0; a < desc->n_axes; ++a) {
+        theta[a] = turn;
+        ratio[a] = desc->per_axis && pairs[a] > 1 ? ratio_of(pairs[a]) : 1;
+    }
+    for (int i = 0; i < half; ++i, all *= ratio_all) {
         const int a = desc->axis_of_pair[i];
         table.axis[i] = (int8_t)a;
         table.turn[i] = 0;
         if (a < 0) continue;
-        const long double power = desc->per_axis ? (long double)seen[a]++ / pairs[a] : (long double)i / half;
-        // theta / 2 pi in units of 2^-64 of a turn (theta <= 1: at most 0.16 of the range); the 64 bits of the format's mantissa are all used
-        const long double inv_2pi = 0.159154943091895335768883763372514362L;
-        table.turn[i] = (uint64_t)roundl(ldexpl(powl((long double)desc->base, -power) * inv_2pi, 64));
+        table.turn[i] = (uint64_t)((desc->per_axis ? theta[a] : all) + 0.5L);
+        theta[a] *= ratio[a];
     }
     return OB_OK;
 }
