@@ -139,7 +139,7 @@ int ob_varlen_attn_bwd_static(const void *d_o, const void *q, const void *k, con
  * tiles that no row of a workgroup sees are not computed, so a call costs tokens * window, not tokens^2.  Nothing of another segment is
  * read on a segment's behalf; inside a segment an infinity or NaN in a row of k, v or d_o may also reach rows near it that do not see it.
  * The backward's workspace (ob_varlen_attn_window_bwd_workspace_bytes for the same arguments; 0 if they are refused) holds the
- * row statistics and, for the sinks of segments longer than the window, the fp32 sums over chunks of their queries, which are
+ * row statistics and, for the sinks of segments much longer than the window, the fp32 sums over chunks of their queries, which are
  * added in order: no atomics, results are bitwise reproducible. */
 int ob_varlen_attn_window_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
                               const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, int dtype,

@@ -337,17 +337,29 @@ __device__ __forceinline__ TileInfo pick_tile(const TileOrder &ord, int rank, co
 
 // What a causal row sees of the keys in front of it: all of its segment, or with a window the last `window` keys (its own
 // among them) and the segment's first `sinks`.  Of dK / dV the two parts of a windowed launch differ: Band owns tiles of key rows and
-// walks the queries whose window reaches them, Sinks owns the first keys of a segment longer than the window, which every row sees, and a
-// chunk of the segment's queries (see launch_attn_window_bwd()).
+// walks the queries whose window reaches them, in a segment's first tile up to `whole` rows all of them; Sinks owns the first keys of a longer segment,
+// which every row sees, and a chunk of its queries (see launch_attn_window_bwd()).
 // A windowed launch loads nothing of another segment (rows past the end of its own arrive as zeros): no value there, infinite or
 // not a number, can reach it.
 struct Whole { static constexpr bool BAND = false, SINKS = false; };
-struct Band { static constexpr bool BAND = true, SINKS = false; int window, sinks; };
-struct Sinks { static constexpr bool BAND = false, SINKS = true; int window, sinks, chunk; float *part; };
+struct Band { static constexpr bool BAND = true, SINKS = false; int window, sinks, whole; };      // whole: see sink_whole_rows()
+struct Sinks { static constexpr bool BAND = false, SINKS = true; int whole, sinks, chunk; float *part; };
 
 // ------------------------------------------------------------------------------------------------
 // forward:  S^T = K Q^T,  online softmax per lane,  O^T += V^T P^T
 // ------------------------------------------------------------------------------------------------
+// The masks of dK / dV in windowed launches are worked out as bits, 64 streamed rows to a lane, and go into the scores as what their accumulators start
+// from: 0, or so large a negative number that a score added to it is lost (two instructions per score, in front of the products, where the lane waits for its
+// operands, instead of four behind them: 8192 tokens, 32 / 8 heads of 128, window 1024 316 -> 307 us, 128 129 -> 124; the forward and dQ gain nothing).
+// bits [first, last] of 64, both any int
+__device__ __forceinline__ uint64_t bit_range(int first, int last) {
+    const uint64_t upto = last >= 63 ? ~0ull : last < 0 ? 0ull : (2ull << last) - 1;
+    return first <= 0 ? upto : first > 63 ? 0ull : upto & (~0ull << first);
+}
+__device__ __forceinline__ float start_of(uint32_t hidden, int c) {
+    return __int_as_float(__builtin_amdgcn_sbfe((int)hidden, c, 1) & __float_as_int(NEG_BIG));
+}
+
 // The key tiles that a workgroup of 128 query rows walks.  With a window: the segment's first tile for the sinks, where the band does not start
 // in it, then those of the band; n_head tiles from the start need a mask, as some row's window begins in or behind them, and `skip` tiles
 // of the segment in front of the band are left out.
@@ -374,7 +386,7 @@ struct BandTiles<Band> {
         n_head = min(whole, (last + ST) / ST) - skip;
     }
     __device__ __forceinline__ int row(int j) const { return (apart && j == 0 ? 0 : j + skip) * ST; }
-    __device__ __forceinline__ bool wave_sees(int kv_first, int rows) const { return kv_first + rows > wave_from; }
+    __device__ __forceinline__ bool wave_sees(int kv_first, int rows) const { return kv_first + rows > wave_from || kv_first < sink_end; }
 };
 
 // LDS reads are issued one batch ahead of the MFMAs that consume them (explicit double buffers and
@@ -387,9 +399,9 @@ struct BandTiles<Band> {
         __builtin_amdgcn_sched_barrier(0);                         \
     } while (0)
 
-// BAND: a row sees its last `window` keys; SINK: and the tile's keys below sink_end.  As an unsigned number the distance from key to row is below the
+// BAND: a row sees its last `window` keys and those below sink_end.  As an unsigned number the distance from key to row is below the
 // window for just the keys of the band, those behind the row and past the segment's end left out: one comparison.
-template <int D, bool CAUSAL, bool MASK, bool BAND = false, bool SINK = false>
+template <int D, bool CAUSAL, bool MASK, bool BAND = false>
 __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict__ ks,
                                          const unsigned char OB_LDS *__restrict__ vs, const Tile<D> &tl,
                                          const bf16x8 (&qf)[D / 16], f32x16 (&acc_o)[D / 32], float &m_run,
@@ -438,7 +450,7 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
             for (int r = 0; r < 16; ++r) {
                 const int kv = kv0 + mt * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
                 const int c = mt * 32 + 8 * (r >> 2) + (r & 3);
-                const bool ok = BAND ? (unsigned)(dist - c) < (unsigned)window || (SINK && c < below) : kv < seg_end && (!CAUSAL || kv <= q_row);
+                const bool ok = BAND ? (unsigned)(dist - c) < (unsigned)window || c < below : kv < seg_end && (!CAUSAL || kv <= q_row);
                 const float s = ok ? acc_s[mt][r] : NEG_BIG;
                 acc_s[mt][r] = s;
                 mx = fmaxf(mx, s);
@@ -577,15 +589,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
         if (!(MASKED))                                                                                   \
             fwd_tile<D, CAUSAL, false>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0, ti.seg_end, q_row,  \
                                        sl2);                                                             \
-        else if (!(CAUSAL && kv0 > wave_q_last)) {                                                       \
-            if (WIN::BAND && kv0 < bt.sink_end)                                                          \
-                fwd_tile<D, CAUSAL, true, WIN::BAND, WIN::BAND>((KS), (VS), tl, qf, acc_o, m_run, l_run, \
-                                                                kv0, ti.seg_end, q_row, sl2, bt.window,  \
-                                                                bt.sink_end);                            \
-            else if (bt.wave_sees(kv0, ST))                                                              \
-                fwd_tile<D, CAUSAL, true, WIN::BAND>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0,       \
-                                                     ti.seg_end, q_row, sl2, bt.window);                 \
-        }                                                                                                \
+        else if (!(CAUSAL && kv0 > wave_q_last) && bt.wave_sees(kv0, ST))                                \
+            fwd_tile<D, CAUSAL, true, WIN::BAND>((KS), (VS), tl, qf, acc_o, m_run, l_run, kv0,           \
+                                                 ti.seg_end, q_row, sl2, bt.window, bt.sink_end);        \
         ++j;                                                                                             \
     }
 #define OB_FWD_ANY(MASKED) OB_FWD_ITER(MASKED, (j & 1) ? ks1 : ks0, (j & 1) ? vs1 : vs0, (j & 1) ? ks0 : ks1, (j & 1) ? vs0 : vs1)
@@ -631,7 +637,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
 // on one half of the tile with their partial dQ added at the end, asked the L2 for twice the bytes
 // per MFMA (4.7 GB per launch on the 7B-shaped batch, 10 TB/s) and had a barrier per 24 MFMAs.
 // ------------------------------------------------------------------------------------------------
-template <int D, bool CAUSAL, bool MASK, bool BAND = false, bool SINK = false>
+template <int D, bool CAUSAL, bool MASK, bool BAND = false>
 __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__ ks,
                                         const unsigned char OB_LDS *__restrict__ vs, const Tile<D> &tl,
                                         const bf16x8 (&qf)[D / 16], const bf16x8 (&dof)[D / 16],
@@ -681,9 +687,8 @@ __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__
             const int r = 8 * h + e;
             bool ok = true;
             if (MASK) {
-                const int kv = kv_first + 8 * (r >> 2) + 4 * lh + (r & 3);
-                const int c = 8 * (r >> 2) + (r & 3);
-                ok = BAND ? (unsigned)(dist - c) < (unsigned)window || (SINK && c < below) : kv < seg_end && (!CAUSAL || kv <= q_row);
+                const int kv = kv_first + 8 * (r >> 2) + 4 * lh + (r & 3), c = 8 * (r >> 2) + (r & 3);
+                ok = BAND ? (unsigned)(dist - c) < (unsigned)window || c < below : kv < seg_end && (!CAUSAL || kv <= q_row);
             }
             const float p = ok ? fast_exp2(acc_s[r] * sl2 - lse2) : 0.f;
             o[e] = (__bf16)(p * (acc_dp[r] - dlt));
@@ -798,16 +803,11 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
                 if (wave_live)                                                                               \
                     dq_half<D, CAUSAL, false>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, acc_dq, lse2,  \
                                               dlt, kv_first, ti.seg_end, q_row, sl2);                        \
-            } else if (wave_live && kv_first < ti.seg_end && !(CAUSAL && kv_first > wave_q_last)) {          \
-                if (WIN::BAND && kv_first < bt.sink_end)                                                     \
-                    dq_half<D, CAUSAL, true, WIN::BAND, WIN::BAND>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, \
-                                                                   acc_dq, lse2, dlt, kv_first, ti.seg_end,  \
-                                                                   q_row, sl2, bt.window, bt.sink_end);      \
-                else if (bt.wave_sees(kv_first, 32))                                                         \
-                    dq_half<D, CAUSAL, true, WIN::BAND>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof,     \
-                                                        acc_dq, lse2, dlt, kv_first, ti.seg_end, q_row, sl2, \
-                                                        bt.window);                                          \
-            }                                                                                                \
+            } else if (wave_live && kv_first < ti.seg_end && !(CAUSAL && kv_first > wave_q_last) &&          \
+                       bt.wave_sees(kv_first, 32))                                                           \
+                dq_half<D, CAUSAL, true, WIN::BAND>((KS) + hf * HALF, (VS) + hf * HALF, tl, qf, dof, acc_dq,  \
+                                                    lse2, dlt, kv_first, ti.seg_end, q_row, sl2, bt.window,  \
+                                                    bt.sink_end);                                            \
         }                                                                                                    \
         ++j;                                                                                                 \
     }
@@ -853,14 +853,15 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
 // of 7168 2.9 %, both builds in turn; a fixed priority for either role loses, the forward and dQ gain nothing).
 // ------------------------------------------------------------------------------------------------
 // scores of a streamed tile of 32 MT rows against the 32 held rows: acc[mt] = rows 32 mt .. of the tile
-template <int D, int MT>
+// (HIDE: `hidden` says which of them the lane's row does not see)
+template <int D, int MT, bool HIDE = false>
 __device__ __forceinline__ void dkv_scores(const unsigned char OB_LDS *__restrict__ tile, const Tile<D, 32 * MT> &tl,
-                                           const bf16x8 (&held)[D / 16], f32x16 (&acc)[MT]) {
+                                           const bf16x8 (&held)[D / 16], f32x16 (&acc)[MT], uint64_t hidden = 0) {
     constexpr int HB = D / 32, NB = MT * (D / 16) / HB, PER = NB / MT;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[mt][r] = 0.f;
+        for (int r = 0; r < 16; ++r) acc[mt][r] = HIDE ? start_of((uint32_t)(hidden >> (32 * mt)), 8 * (r >> 2) + (r & 3)) : 0.f;
     bf16x8 fr[2][HB];
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -883,10 +884,9 @@ __device__ __forceinline__ void dkv_scores(const unsigned char OB_LDS *__restric
 
 // role P: probabilities of the 32 MT x 32 score tile, packed as the second operands of the 2 MT
 // 16-row contraction steps (pk[mt][h] serves step 2 mt + h)
-// (SPAN: the rows that see the key are the `span` from its own on)
-template <bool CAUSAL, bool MASK, int MT, bool SPAN = false>
+template <bool CAUSAL, bool MASK, int MT>
 __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned char OB_LDS *__restrict__ lse2_s,
-                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2], int span = 0) {
+                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2]) {
     const int lh = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -899,7 +899,7 @@ __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned 
                 bool ok = true;
                 if (MASK) {
                     const int qr = q0 + mt * 32 + 8 * g + 4 * lh + e;
-                    ok = SPAN ? (unsigned)(qr - kv_row) < (unsigned)span : qr < seg_end && (!CAUSAL || kv_row <= qr);
+                    ok = qr < seg_end && (!CAUSAL || kv_row <= qr);
                 }
                 const float pe = fast_exp2(s[mt][4 * g + e] * sl2 - l4[e]);
                 p[4 * g + e] = ok ? pe : 0.f;
@@ -1083,11 +1083,21 @@ struct DkvWalk {
         n_masked = group * (n_diag + n_end);
         n_all = n_masked + group * n_mid;
     }
-    // Rows [q_begin, q_end), `head` masked tiles in front, the first `free_rows` rows otherwise without a mask
-    __device__ __forceinline__ DkvWalk(int q_begin_, int q_end, int head, int free_rows, int group) : q_begin(q_begin_), dead(0) {
+    // with a window: up to row q_end; the whole's first `free_rows` rows are in every key's window
+    __device__ __forceinline__ DkvWalk(const TileInfo &ti, int q_end, int free_rows, int group) {
+        q_begin = ti.row0 - (ti.row0 - ti.seg_start) % WHOLE;
+        dead = (ti.row0 - q_begin) / SR;
+        set(q_end, WHOLE / SR, free_rows, group);
+    }
+    // the sinks: a chunk of rows from q_begin on, all of a segment's rows in front of it done by others
+    __device__ __forceinline__ DkvWalk(int q_begin_, int q_end, bool diagonal, int group) : q_begin(q_begin_), dead(0) {
+        set(q_end, diagonal ? KVT / SR : 0, q_end - q_begin, group);
+    }
+    __device__ __forceinline__ void set(int q_end, int head, int free_rows, int group) {
         const int n_iter = (q_end - q_begin + SR - 1) / SR;
-        n_head = n_diag = min(head, n_iter);
-        const int n_mid_end = max(n_head, free_rows / SR);
+        n_head = min(head, n_iter);
+        const int n_mid_end = max(n_head, free_rows / DKV_ORDER_Q * (DKV_ORDER_Q / SR));
+        n_diag = n_head - dead;
         n_end = n_iter - n_mid_end;
         n_mid = n_mid_end - n_head;
         n_masked = group * (n_diag + n_end);
@@ -1171,6 +1181,34 @@ struct DkvRequests {
     }
 };
 
+// The rows that see a workgroup's keys: up to q_end; `span` of them from the lane's own key on, none from `past` on the wave's.  sinks_here: the tile has
+// the sinks of a segment without chunks, which see them all.
+template <class WIN>
+struct BandRows {
+    static constexpr int q_end = 0, free_rows = 0, past = 0;
+    static constexpr bool skip = false;
+    __device__ __forceinline__ BandRows(const TileInfo &, const WIN &, int, int, int, int) {}
+    __device__ __forceinline__ uint64_t hidden(int, int, int) const { return 0; }
+};
+template <>
+struct BandRows<Band> {
+    int q_end, free_rows, span, past;
+    bool skip;       // the lane's key is a sink of a segment with chunks: its sums come from those
+    __device__ __forceinline__ BandRows(const TileInfo &ti, const Band &win, int kvt, int whole, int wave_kv_first, int kv_row) {
+        const int len = ti.seg_end - ti.seg_start, sink_end = ti.seg_start + win.sinks;
+        const bool sinks_here = ti.row0 == ti.seg_start && win.sinks > 0 && len <= win.whole;
+        q_end = sinks_here ? ti.seg_end : min(ti.seg_end, ti.row0 + kvt - 1 + win.window);
+        const int whole_row0 = ti.row0 - (ti.row0 - ti.seg_start) % whole;
+        free_rows = min(ti.seg_end - whole_row0, win.window);
+        span = sinks_here && kv_row < sink_end ? q_end - kv_row : min(q_end - kv_row, win.window);
+        past = sinks_here && wave_kv_first < sink_end ? q_end : wave_kv_first + 31 + win.window;
+        skip = kv_row < sink_end && len > win.whole;
+    }
+    __device__ __forceinline__ uint64_t hidden(int kv_row, int q0, int first) const {      // of the 64 rows from q0 on, from the `first`
+        return ~bit_range(kv_row - q0, kv_row - q0 + span - 1) >> first;
+    }
+};
+
 template <int D, bool CAUSAL, int NP, int SR, bool APART = false, class WIN = Whole>
 __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 2) void attn_bwd_dkv_kernel(
     const __bf16 *__restrict__ d_o, const __bf16 *__restrict__ q, const __bf16 *__restrict__ k,
@@ -1187,21 +1225,15 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
     __shared__ int sh[8];
     const int rank = blockIdx.x / heads;
     TileInfo ti;
-    int q_chunk = 0, window = 0;      // (Sinks) first of the workgroup's query rows; (Band) the window
+    int q_chunk = 0;          // (Sinks) first of the workgroup's query rows
     if constexpr (WIN::SINKS) {
-        ti = find_tile<true>(cu, n_seg, win.chunk, sh, rank, win.window);
+        ti = find_tile<true>(cu, n_seg, win.chunk, sh, rank, win.whole);
         q_chunk = ti.row0;
         ti.row0 = ti.seg_start;
     } else {
         ti = pick_tile<true>(ord, rank, cu, n_seg, KVT, sh);
         if (ti.row0 < 0) return;
     }
-    int q_end = ti.seg_end, rows_end = T;
-    if constexpr (WIN::BAND) {
-        window = win.window;
-        rows_end = q_end = min(ti.seg_end, ti.row0 + KVT - 1 + window);
-    }
-    if constexpr (WIN::SINKS) rows_end = q_end = min(ti.seg_end, q_chunk + win.chunk);
     // one workgroup per key/value head: the group's query heads run one after another
     const int kvh = head_of_slot(blockIdx.x - rank * heads, heads);
     const int lane = threadIdx.x & 63, lx = lane & 31, lh = lane >> 5;
@@ -1211,8 +1243,11 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
     const int kv_row = min(ti.row0 + pair * 32 + lx, ti.seg_end - 1);
     const bool kv_live = ti.row0 + pair * 32 + lx < ti.seg_end;
     const int pair_kv_first = ti.row0 + pair * 32;
-    const int span = min(q_end - kv_row, WIN::BAND ? window : MAX_TOKENS);
-    auto band_is_past = [&](int q0) __attribute__((always_inline)) { return q0 - (pair_kv_first + 31) >= window; };
+    constexpr bool HIDE = WIN::BAND || WIN::SINKS;
+    const BandRows<WIN> rows(ti, win, KVT, dkv_whole(D), pair_kv_first, kv_row);
+    int q_end = WIN::BAND ? rows.q_end : ti.seg_end;
+    if constexpr (WIN::SINKS) q_end = min(ti.seg_end, q_chunk + win.chunk);
+    const int rows_end = HIDE ? q_end : T;
     const float sl2 = scale * LOG2E;
     constexpr int KT = D / 16, DT = D / 32;
     constexpr bool FUSE = NP == 2 && SR == 64;      // one or two waves to a SIMD: element-wise work between the wave's own products
@@ -1230,9 +1265,9 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
 
     const auto w = [&] {
         if constexpr (WIN::BAND)
-            return DkvWalk<D, CAUSAL, KVT, SR>(ti.row0, q_end, KVT / SR, min(ti.seg_end - ti.row0, win.window), group);
+            return DkvWalk<D, CAUSAL, KVT, SR>(ti, q_end, rows.free_rows, group);
         else if constexpr (WIN::SINKS)
-            return DkvWalk<D, CAUSAL, KVT, SR>(q_chunk, q_end, q_chunk == ti.seg_start ? KVT / SR : 0, q_end - q_chunk, group);
+            return DkvWalk<D, CAUSAL, KVT, SR>(q_chunk, q_end, q_chunk == ti.seg_start, group);
         else
             return DkvWalk<D, CAUSAL, KVT, SR>(ti, group);
     }();
@@ -1289,12 +1324,20 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
         bare_barrier();
         if (GEN) request(NEXT);      // (the masked tiles' trips are short and each takes a descriptor of its own)
         // (GEN: one after the other, each step behind a test)  a masked tile entirely before this pair's keys contributes nothing
-        const bool live = !GEN || (n < w.n_all && !(MASK && CAUSAL && q0 + SR - 1 < pair_kv_first) && !(WIN::BAND && MASK && band_is_past(q0)));
+        bool live = !GEN || (n < w.n_all && !(MASK && CAUSAL && q0 + SR - 1 < pair_kv_first));
+        if constexpr (WIN::BAND && GEN && MASK) live = live && q0 < rows.past;
         unsigned char OB_LDS *const p_new = p_mine + (n & 1) * (NP * PB), *const p_old = p_mine + ((n & 1) ^ 1) * (NP * PB);
         const bool late = !GEN || (RG ? live_prev : owed);
         if constexpr (!RG) {
             f32x16 acc_x[MT];
-            if (live) dkv_scores<D, MT>(tiles + S * BYTES, tl, kvf, acc_x);
+            if (live) {
+                if constexpr (MASK && WIN::BAND)
+                    dkv_scores<D, MT, true>(tiles + S * BYTES, tl, kvf, acc_x, rows.hidden(kv_row, q0, 4 * lh));
+                else if constexpr (MASK && WIN::SINKS)
+                    dkv_scores<D, MT, true>(tiles + S * BYTES, tl, kvf, acc_x, ~bit_range(kv_row - q0, q_end - 1 - q0) >> (4 * lh));
+                else
+                    dkv_scores<D, MT>(tiles + S * BYTES, tl, kvf, acc_x);
+            }
             if (!GEN) request(NEXT);
             if constexpr (FUSE && !GEN) {
                 bf16x8 pn[MT][2];
@@ -1303,7 +1346,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
                 for (int i = 0; i < 2 * MT; ++i) pk[i >> 1][i & 1] = pn[i >> 1][i & 1];
             } else {
                 if (FUSE && late) dkv_outputs<D, MT>(tiles + PREV * BYTES, tl, pk, acc_out);
-                if (live) dkv_probs<CAUSAL, MASK, MT, WIN::BAND || WIN::SINKS>(acc_x, stat + S * 256, q0, ti.seg_end, kv_row, sl2, pk, span);
+                if (live) dkv_probs<CAUSAL, MASK && !HIDE, MT>(acc_x, stat + S * 256, q0, ti.seg_end, kv_row, sl2, pk);
             }
             if (live) {
 #pragma unroll
@@ -1374,10 +1417,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 
                 *(f32x4 *)(dst + dt * 32 + g * 8 + lh * 4) = f32x4{acc_out[dt][4 * g], acc_out[dt][4 * g + 1], acc_out[dt][4 * g + 2], acc_out[dt][4 * g + 3]};
         return;
     }
-    // (the sinks of a segment longer than the window come from the sums over its chunks)
-    if constexpr (WIN::BAND) {
-        if (kv_row - ti.seg_start < win.sinks && ti.seg_end - ti.seg_start > win.window) return;
-    }
+    if (rows.skip) return;
     if (!kv_live) return;
     // dV^T / dK^T of the whole group of query heads sit in the accumulators: one rounding to bf16
     const float out_scale = role_g ? scale : 1.0f;
@@ -1415,13 +1455,13 @@ struct DkvBlocks {
                          LSE_AT = DS_AT + 2 * BUF, DLT_AT = LSE_AT + LSE_STAGES * 256, TOTAL = DLT_AT + DLT_STAGES * 256;
     static_assert(TOTAL + 64 <= 160 * 1024, "LDS");
 };
-template <bool CAUSAL>
+template <bool CAUSAL, class WIN = Whole>
 __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
     const __bf16 *__restrict__ d_o, const __bf16 *__restrict__ q, const __bf16 *__restrict__ k,
     const __bf16 *__restrict__ v, const float *__restrict__ lse2_all, const float *__restrict__ delta,
     __bf16 *__restrict__ dk, __bf16 *__restrict__ dv, int ldq, int ldkv, int ldo,
     const int32_t *__restrict__ cu, int n_seg, int T, int group, float scale, float rot_log2_base, int heads,
-    TileOrder ord, Whole) {
+    TileOrder ord, WIN win) {
     using B = DkvBlocks;
     constexpr int D = B::D, SR = B::SR, KT = D / 16, BUF = B::BUF, LD = Tile<D, SR>::LD;
     __shared__ __attribute__((aligned(1024))) unsigned char lds_s[B::TOTAL];
@@ -1453,7 +1493,12 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc_out[i][r] = 0.f;
-    const DkvWalk<D, CAUSAL, B::KVT, SR> w(ti, group);
+    const BandRows<WIN> rows(ti, win, B::KVT, dkv_whole(D), ti.row0 + b * 32, kv_row);
+    const int rows_end = WIN::BAND ? rows.q_end : T;
+    const auto w = [&] {
+        if constexpr (WIN::BAND) return DkvWalk<D, CAUSAL, B::KVT, SR>(ti, rows.q_end, rows.free_rows, group);
+        else return DkvWalk<D, CAUSAL, B::KVT, SR>(ti, group);
+    }();
 
     auto walk = [&](auto role_tag) __attribute__((always_inline)) {
     constexpr bool RG = decltype(role_tag)::value;
@@ -1465,7 +1510,7 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
     unsigned char OB_LDS *const p_blk = lds + B::P_AT + (b * 2 + a) * B::BLK + lane * 16;       // own block of the scores
     unsigned char OB_LDS *const ds_blk = lds + B::DS_AT + (b * 2 + a) * B::BLK + lane * 16;
     unsigned char OB_LDS *const out_blk = lds + (RG ? B::DS_AT : B::P_AT) + b * 2 * B::BLK + lane * 16;   // the four steps of a result
-    DkvRequests<D, CAUSAL, B::KVT, SR, LD> req(w, RG ? d_o : q, (RG ? (long)ldo : (long)ldq) * 2, RG ? delta : lse2_all, T, T, kvh * group, group,
+    DkvRequests<D, CAUSAL, B::KVT, SR, LD> req(w, RG ? d_o : q, (RG ? (long)ldo : (long)ldq) * 2, RG ? delta : lse2_all, T, rows_end, kvh * group, group,
                                               w4 * LD, tl.voff);
     auto next = [](int stage, int stages) __attribute__((always_inline)) { return stage + 1 == stages ? 0 : stage + 1; };
     int st_issue = 0, st_stat_issue = 0;                                       // stages of the tile to request next
@@ -1504,8 +1549,10 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
         bf16x8 fr[KT], of[4], tf[4][2], pk[2];
         f32x4 row4[4];                                                                // lse2 (P), Delta (G)
         f32x16 s;
+        uint64_t hidden = 0;
+        if constexpr (WIN::BAND && MASK && !RG) hidden = rows.hidden(kv_row, q0, a * 32 + 4 * lh);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 0.f;
+        for (int r = 0; r < 16; ++r) s[r] = WIN::BAND && MASK && !RG ? start_of((uint32_t)hidden, 8 * (r >> 2) + (r & 3)) : 0.f;
         if (has_score) {
 #pragma unroll
             for (int t = 0; t < KT; ++t) fr[t] = lds16<bf16x8>(sc + rr[t]);
@@ -1546,7 +1593,7 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
                         pk[h][e] = (__bf16)((float)pk[h][e] * (dp_keep[r] - row4[g][r & 3]));
                     } else {
                         const int qr = q0 + a * 32 + 8 * g + 4 * lh + (r & 3);
-                        const bool ok = !MASK || (qr < ti.seg_end && (!CAUSAL || kv_row <= qr));
+                        const bool ok = !MASK || WIN::BAND || (qr < ti.seg_end && (!CAUSAL || kv_row <= qr));
                         const float p = fast_exp2(s[r] * sl2 - row4[g][r & 3]);
                         pk[h][e] = (__bf16)(ok ? p : 0.f);
                     }
@@ -1589,6 +1636,7 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
     while (n < w.n_all + 2) trip(std::true_type{}, std::false_type{});
     };
     if (role_g) walk(std::true_type{}); else walk(std::false_type{});
+    if (rows.skip) return;
     if (!kv_live) return;
     const float out_scale = role_g ? scale : 1.0f;
     __bf16 *const dst = role_g ? dk : dv;
@@ -1604,22 +1652,29 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
         }
 }
 
-// dK and dV of the sinks of every segment longer than the window: the fp32 sums of its chunks, in order, then one rounding.  Workgroups
-// (place, key/value head, 256 elements), those of a segment's first chunk at work; a wave adds a quarter of the chunks.
+// dK and dV of the sinks of every segment with chunks: the chunks' fp32 sums in order, then one rounding.  Workgroups (segment with chunks, key/value head,
+// 256 elements); a wave adds a quarter of the chunks.
 template <int D>
 __global__ __launch_bounds__(256) void attn_sink_sum_kernel(const float *__restrict__ part, __bf16 *__restrict__ dk, __bf16 *__restrict__ dv,
                                                             int ldkv, const int32_t *__restrict__ cu, int n_seg, Sinks win, float scale) {
     __shared__ int sh[8];
     __shared__ f32x4 quarter[4][64];
-    const int place = blockIdx.x, kvh = blockIdx.y, nkv = gridDim.y;
-    const TileInfo ti = find_tile<true>(cu, n_seg, win.chunk, sh, place, win.window);
-    if (ti.row0 != ti.seg_start) return;
-    const int len = ti.seg_end - ti.seg_start, chunks = (len + win.chunk - 1) / win.chunk;
+    const int kvh = blockIdx.y, nkv = gridDim.y;
+    const TileInfo ti = find_tile<true>(cu, n_seg, MAX_TOKENS, sh, blockIdx.x, win.whole);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (blockIdx.z * 64 + lane) * 4;
+    // chunks of the segments in front of it
+    int slot0 = 0;
+    for (int j = lane; j < n_seg && cu[j] < ti.seg_start; j += 64) {
+        const int n = cu[j + 1] - cu[j];
+        slot0 += n > win.whole ? (n + win.chunk - 1) / win.chunk : 0;
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) slot0 += __shfl_xor(slot0, o);
+    const int len = ti.seg_end - ti.seg_start, chunks = (len + win.chunk - 1) / win.chunk;
     const int role = e / (win.sinks * D), r = e - role * win.sinks * D;
     const bool live = role < 2 && r / D < len;
     const size_t slot = (size_t)nkv * 2 * win.sinks * D;
-    const float *src = part + (size_t)place * slot + (size_t)kvh * 2 * win.sinks * D + e;
+    const float *src = part + (size_t)slot0 * slot + (size_t)kvh * 2 * win.sinks * D + e;
     const int per = (chunks + 3) / 4, end = min(chunks, (wave + 1) * per);
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     if (live) {
@@ -1700,8 +1755,8 @@ OB_ATTN_INSTANCES(128, false)
                                                                float *, float *, __bf16 *, int, int, int,          \
                                                                const int32_t *, int, int, int, float, float, int,  \
                                                                TileOrder, Band);                                   \
-    OB_WINDOW_DKV(D, Band, window_np(D), window_sr(D))                                                              \
-    OB_WINDOW_DKV(D, Sinks, 2, window_sr(D))                                                                        \
+    OB_WINDOW_DKV(D, Band, dkv_np(D, 0), dkv_sr(D, 0))                                                              \
+    OB_WINDOW_DKV(D, Sinks, 2, dkv_sr(D, 1))                                                                        \
     template __global__ void attn_sink_sum_kernel<D>(const float *, __bf16 *, __bf16 *, int, const int32_t *, int, Sinks, float);
 #define OB_WINDOW_DKV(D, W, NP, SR)                                                                               \
     template __global__ void attn_bwd_dkv_kernel<D, true, NP, SR, false, W>(const __bf16 *, const __bf16 *, const __bf16 *, \
@@ -1711,6 +1766,10 @@ OB_ATTN_INSTANCES(128, false)
                                                            TileOrder, W);
 OB_WINDOW_INSTANCES(64)
 OB_WINDOW_INSTANCES(128)
+OB_WINDOW_DKV(64, Band, dkv_np(64, 1), dkv_sr(64, 1))
+template __global__ void attn_bwd_dkv_blocks_kernel<true, Band>(const __bf16 *, const __bf16 *, const __bf16 *, const __bf16 *, const float *,
+                                                                const float *, __bf16 *, __bf16 *, int, int, int, const int32_t *, int, int, int,
+                                                                float, float, int, TileOrder, Band);
 #undef OB_WINDOW_DKV
 #undef OB_WINDOW_INSTANCES
 OB_BLOCKS_INSTANCE(true)
@@ -1796,15 +1855,14 @@ void launch_attn_window_fwd(const void *q, const void *k, const void *v, void *o
     const int tiles = make_order(seg, QT, true, false, ord, window);
     const dim3 grid((unsigned)tiles * nq);
 #define OB_ARGS (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, (__bf16 *)o, lse, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, \
-                seg->total_tokens, nq / nkv, scale, nq, ord, Band{window, sinks}
+                seg->total_tokens, nq / nkv, scale, nq, ord, Band{window, sinks, 0}
     if (d == 64) hipLaunchKernelGGL((attn_fwd_kernel<64, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
     else hipLaunchKernelGGL((attn_fwd_kernel<128, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
 #undef OB_ARGS
 }
 
-// dQ; dK and dV of the keys that leave the window, by tiles of key rows; those of the sinks of segments longer than it, which every
-// row sees: a tile of key rows that walked all of a long segment would keep the launch waiting, so chunks of the queries leave
-// fp32 sums in `part` and a last launch adds them in order.
+// dQ; dK and dV by tiles of key rows; those of the sinks of longer segments, which every row sees, apart: a tile of key rows that walked all of a long
+// segment would keep the launch waiting, so chunks of the queries leave fp32 sums in `part` and a last launch adds them in order.
 void launch_attn_window_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
                             float *lse2, float *delta, float *part, void *dq, void *dk, void *dv, int ldq, int ldkv, int ldo,
                             const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s) {
@@ -1813,32 +1871,36 @@ void launch_attn_window_bwd(const void *d_o, const void *q, const void *k, const
     TileOrder ord;
     {
         ProfScope prof(K_ATTN_BWD_DQ, s, 0.5 * flops);
-        const int tiles = make_order(seg, QT, true, false, ord, window);
+        int tiles = make_order(seg, QT, true, false, ord, window);
         const dim3 grid((unsigned)tiles * nq);
 #define OB_ARGS (const __bf16 *)d_o, (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, (const __bf16 *)o, lse, lse2, delta,  \
-                (__bf16 *)dq, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, group, scale, 0.f, nq, ord, Band{window, sinks}
+                (__bf16 *)dq, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, group, scale, 0.f, nq, ord, Band{window, sinks, 0}
         if (d == 64) hipLaunchKernelGGL((attn_bwd_dq_kernel<64, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
         else hipLaunchKernelGGL((attn_bwd_dq_kernel<128, true, Band>), grid, dim3(256), 0, s, OB_ARGS);
 #undef OB_ARGS
     }
     ProfScope prof(K_ATTN_BWD_DKV, s, 1.5 * flops);
-    const int places = make_order(seg, 32 * window_np(d), true, true, ord, window), threads = 128 * window_np(d);
+    const int whole = sink_whole_rows(window, group), shape = dkv_shape(seg, nkv, group, d, true, window, sinks ? whole : 0);
+    const int places = make_order(seg, 32 * dkv_np(d, shape), true, true, ord, window, sinks ? whole : 0), threads = dkv_threads(d, shape);
 #define OB_ARGS(W) (const __bf16 *)d_o, (const __bf16 *)q, (const __bf16 *)k, (const __bf16 *)v, lse2, delta, (__bf16 *)dk, (__bf16 *)dv,  \
                    ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, group, scale, 0.f, nkv, ord, W
     const dim3 grid((unsigned)places * nkv);
-    const Band band{window, sinks};
-    if (d == 64) hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, window_np(64), window_sr(64), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
-    else hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, window_np(128), window_sr(128), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
-    const int chunks = sink_chunks(seg, d, window, sinks);
+    const Band band{window, sinks, whole};
+    if (d == 64 && shape == 0) hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, dkv_np(64, 0), dkv_sr(64, 0), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
+    else if (d == 64) hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, dkv_np(64, 1), dkv_sr(64, 1), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
+    else if (shape == 0) hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, dkv_np(128, 0), dkv_sr(128, 0), false, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
+    else hipLaunchKernelGGL((attn_bwd_dkv_blocks_kernel<true, Band>), grid, dim3(threads), 0, s, OB_ARGS(band));
+    int split;
+    const int chunks = sink_chunks(seg, whole, sinks, &split);
     if (!chunks) return;
-    const Sinks first{window, sinks, sink_chunk_rows(d), part};
-    const dim3 grid_s((unsigned)chunks * nkv), grid_r(chunks, nkv, (2 * sinks * d + 255) / 256);
+    const Sinks first{whole, sinks, SINK_CHUNK, part};
+    const dim3 grid_s((unsigned)chunks * nkv), grid_r(split, nkv, (2 * sinks * d + 255) / 256);
     ord.n = 0;
     if (d == 64) {
-        hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, 2, window_sr(64), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
+        hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, 2, dkv_sr(64, 1), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
         hipLaunchKernelGGL((attn_sink_sum_kernel<64>), grid_r, dim3(256), 0, s, part, (__bf16 *)dk, (__bf16 *)dv, ldkv, seg->cu_dev, seg->n_seg, first, scale);
     } else {
-        hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, 2, window_sr(128), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
+        hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, 2, dkv_sr(128, 1), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
         hipLaunchKernelGGL((attn_sink_sum_kernel<128>), grid_r, dim3(256), 0, s, part, (__bf16 *)dk, (__bf16 *)dv, ldkv, seg->cu_dev, seg->n_seg, first, scale);
     }
 #undef OB_ARGS

@@ -25,7 +25,7 @@ int count_tiles(const ob_segments *seg, int tile_rows) {
 // the workgroup owns key rows and streams query tiles (from its diagonal on when causal); otherwise
 // it owns query rows and streams key tiles (up to its diagonal when causal).  A unit counts as its first
 // tile, on the key side the heaviest of them.  No heap memory.
-int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window) {
+int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window, int whole) {
     ord.n = ord.unit_log2 = 0;
     const int n_tiles = count_tiles(seg, tile_rows), max_log2 = kv_side && tile_rows == 64 ? 2 : 0;
     int log2 = 0, n_units = n_tiles;
@@ -42,7 +42,7 @@ int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side,
             int rows = len;                                            // streamed rows
             if (causal && kv_side) rows = len - (t * unit_rows) / ST * ST;
             else if (causal) rows = std::min(len, (t + 1) * unit_rows);
-            if (window) rows = std::min(rows, window + unit_rows);
+            if (window && !(kv_side && t == 0 && len <= whole)) rows = std::min(rows, window + unit_rows);
             const uint32_t w = (uint32_t)((rows + ST - 1) / ST);
             // ascending sort of (~work, natural index); the entry rides in the low half
             key[n] = ((uint64_t)(0xFFFFFu - w) << 44) | ((uint64_t)n << 32) | ((uint32_t)j << 16) | (uint32_t)t;
@@ -56,14 +56,15 @@ int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side,
     return n << log2;
 }
 
-int sink_chunks(const ob_segments *seg, int d, int window, int sinks) {
-    if (!sinks) return 0;
-    const int rows = sink_chunk_rows(d);
-    int n = 0;
-    for (int j = 0; j < seg->n_seg; ++j) {
+int sink_chunks(const ob_segments *seg, int whole, int sinks, int *segments) {
+    int n = 0, split = 0;
+    for (int j = 0; j < seg->n_seg && sinks; ++j) {
         const int len = seg->cu_host[j + 1] - seg->cu_host[j];
-        if (len > window) n += (len + rows - 1) / rows;
+        if (len <= whole) continue;
+        n += (len + SINK_CHUNK - 1) / SINK_CHUNK;
+        ++split;
     }
+    if (segments) *segments = split;
     return n;
 }
 
@@ -81,7 +82,7 @@ struct DkvShape { int kv_rows; double full, chain, ends; };
 constexpr DkvShape DKV_64[] = {{64, 0.81, 1.1, 0}, {64, 0.70, 1.53, 0}};                                // SR = 64, SR = 32 (six pairs: below)
 constexpr DkvShape DKV_128[] = {{128, 1.69, 2.5, 0}, {64, 2.4, 0.85, 1.5}, {64, 2.8, 1.25, 0}};      // four pairs, blocks, two pairs
 }  // namespace
-int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal) {
+int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal, int window, int whole) {
     int best = 0;
     double t_best = 0;
     for (int i = 0; i < (d == 128 && !causal ? 3 : 2); ++i) {      // (shape 2 is bidirectional)
@@ -89,6 +90,12 @@ int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal) {
         double sum = 0, chain = 0;
         for (int j = 0; j < seg->n_seg; ++j) {
             const double len = seg->cu_host[j + 1] - seg->cu_host[j], tiles = ceil(len / sh.kv_rows), first = ceil(len / 64);
+            if (window && len > window) {      // a tile's walk is cut off behind the window
+                const double walk = ceil((window + sh.kv_rows) / 64.0), full = std::max(0.0, tiles - ceil(walk * 64 / sh.kv_rows)), rest = tiles - full;
+                sum += full * walk + 0.5 * rest * (rest + 1) * sh.kv_rows / 64;
+                chain = std::max(chain, len <= whole ? first : std::min(walk, first));
+                continue;
+            }
             sum += tiles * first - (causal ? 0.5 * tiles * (tiles - 1) * sh.kv_rows / 64 : 0.0);
             chain = std::max(chain, first);
         }

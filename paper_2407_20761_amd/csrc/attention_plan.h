@@ -48,16 +48,16 @@ __host__ __device__ constexpr bool dkv_tile_fits(uint32_t ld2, int sr) { return 
 __host__ __device__ constexpr uint32_t dkv_piece_offset(uint32_t voff, uint32_t row, uint32_t ld2) { return voff - row * ld2; }
 
 // the order of a launch; returns its places (workgroups per head): as many as tiles, or whole units of them
-// (window > 0: causal, a row sees no more than that many keys)
-int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window = 0);
-int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal);
+// (window > 0: causal, a row sees no more than that many keys; the first tile of key rows of a segment of up to `whole` is seen by all its rows)
+int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window = 0, int whole = 0);
+int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal, int window = 0, int whole = 0);
 
-// Windowed attention: dK / dV in pairs of 32 key rows and query tiles, as above
-constexpr int window_np(int d) { return d == 64 ? 2 : 4; }
-constexpr int window_sr(int d) { return d == 64 ? 32 : 64; }
-// Rows of a chunk of queries that the sinks' sums are split into (of its own: not of the batch, so that a segment gives the same sums in every batch), and
-// how many such chunks the segments longer than the window have
-constexpr int sink_chunk_rows(int d) { return d == 64 ? 256 : 256; }
-int sink_chunks(const ob_segments *seg, int d, int window, int sinks);
+// The sinks of a segment are seen by all of its rows.  Up to sink_whole_rows() the workgroup of its first keys walks them all: what that adds to its
+// walk, rows past the window times the heads of a group, is to cost less than the two launches of the other way (about 25 trips of 64 rows).
+// Beyond, chunks of SINK_CHUNK rows leave fp32 sums.  Both are the segment's own, so that it gives the same sums in every batch.
+constexpr int SINK_CHUNK = 256;
+constexpr int sink_whole_rows(int window, int group) { return window + 1600 / group; }
+// chunks of all the segments that have them, and how many segments that are
+int sink_chunks(const ob_segments *seg, int whole, int sinks, int *segments = nullptr);
 
 }  // namespace ob

@@ -28,7 +28,7 @@ struct WindowWork { size_t delta, lse2, part, total; };
 WindowWork work_layout(const ob_segments *seg, int nq, int nkv, int d, int window, int sinks, int dtype) {
     const size_t rows = align_up((size_t)seg->total_tokens * nq * 4, 256);
     WindowWork w{0, rows, 2 * rows, rows};
-    if (dtype == OB_BF16) w.total = w.part + align_up((size_t)sink_chunks(seg, d, window, sinks) * nkv * 2 * sinks * d * 4, 256);
+    if (dtype == OB_BF16) w.total = w.part + align_up((size_t)sink_chunks(seg, sink_whole_rows(window, nq / nkv), sinks) * nkv * 2 * sinks * d * 4, 256);
     return w;
 }
 
