@@ -228,6 +228,11 @@ int ob_varlen_attn_bwd_plan(const ob_segments *seg, int nq, int nkv, int d, int 
  * two pairs of waves. */
 int ob_varlen_attn_bwd_threads(const ob_segments *seg, int nq, int nkv, int d, int mask, int *threads);
 
+/* Host only, for tests: the dK / dV launch of ob_varlen_attn_window_bwd (bf16; its shape as in ob_varlen_attn_bwd_plan, its threads) and the
+ * chunks of queries that the sinks' sums take (0: none). */
+int ob_varlen_attn_window_bwd_plan(const ob_segments *seg, int nq, int nkv, int d, int window, int sinks, ob_attn_bwd_launch *launch,
+                                   int *threads, int *chunks);
+
 /* ---- ViT -> LLM hand-over of a mixed stage (App. A; the "token sub-sampling" of Sec. 5.4) ------
  * The paper names the step but fixes neither it nor the connector; what runs here is
  *   c1  per tile of grid*grid + 1 ViT rows (class token first, patches row-major): drop the class
@@ -311,6 +316,24 @@ typedef struct {
 } ob_rotary_axes_desc;
 int ob_rotary_axes(const ob_rotary_axes_desc *desc, const void *x, int ldx, void *y, int ldy, int total_tokens, int n_heads,
                    const int32_t *pos, int inverse, int dtype, void *hip_stream);
+
+/* ---- a block with these in its attention ----------------------------------------------------------
+ * The block of `desc` with a window (0: none; else the mask has to be causal) and sinks as in ob_varlen_attn_window_fwd, and
+ * with `rotary` (NULL: as desc says) rotary positions of several axes on its query and key heads (desc->use_rotary 0; pos:
+ * device memory, [n_axes][total_tokens]).  Everything else as ob_block_fwd / ob_block_bwd, `saved` (ob_block_saved_bytes) and
+ * ob_block_saved_offset among it; the workspace of the backward is ob_block_attn_workspace_bytes (0: refused arguments), of
+ * the forward ob_block_workspace_bytes will do. */
+typedef struct {
+    int window, sinks;
+    const ob_rotary_axes_desc *rotary;
+    const int32_t *pos;
+} ob_block_attn;
+size_t ob_block_attn_workspace_bytes(const ob_block_desc *desc, const ob_block_attn *attn, const ob_segments *seg);
+int ob_block_attn_fwd(const ob_block_desc *desc, const ob_block_attn *attn, const ob_block_weights *w, const void *x, void *y,
+                      void *saved, size_t saved_bytes, const ob_segments *seg, void *ws, size_t ws_bytes, void *hip_stream);
+int ob_block_attn_bwd(const ob_block_desc *desc, const ob_block_attn *attn, const ob_block_weights *w, const ob_block_grads *g,
+                      int flags, const void *x, const void *dy, void *dx, void *saved, size_t saved_bytes,
+                      const ob_segments *seg, void *ws, size_t ws_bytes, void *hip_stream);
 
 /* T x T byte mask (1 = allowed): allowed(i, j) <=> i and j lie in the same segment (and j <= i when
  * causal), evaluated per entry from cu_seqlens by a small kernel of its own (the attention kernels

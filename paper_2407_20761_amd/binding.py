@@ -68,6 +68,10 @@ class ob_rotary_axes_desc(C.Structure):
     _fields_ = [("head_dim", C.c_int), ("n_axes", C.c_int), ("base", C.c_float), ("per_axis", C.c_int), ("axis_of_pair", C.c_int8 * 64)]
 
 
+class ob_block_attn(C.Structure):
+    _fields_ = [("window", C.c_int), ("sinks", C.c_int), ("rotary", C.POINTER(ob_rotary_axes_desc)), ("pos", C.c_void_p)]
+
+
 CONNECTOR_FIELDS = ("n_g", "n_b", "w1", "b1", "w2", "b2")
 
 
@@ -120,6 +124,11 @@ _SIGNATURES = {
     "ob_block_fwd": (_I, [_DESC, C.POINTER(ob_block_weights), _P, _P, _P, _Z, _SEG, _P, _Z, _P]),
     "ob_block_bwd": (_I, [_DESC, C.POINTER(ob_block_weights), C.POINTER(ob_block_grads), _I, _P, _P,
                           _P, _P, _Z, _SEG, _P, _Z, _P]),
+    "ob_block_attn_workspace_bytes": (_Z, [_DESC, C.POINTER(ob_block_attn), _SEG]),
+    "ob_block_attn_fwd": (_I, [_DESC, C.POINTER(ob_block_attn), C.POINTER(ob_block_weights), _P, _P, _P, _Z, _SEG, _P, _Z, _P]),
+    "ob_block_attn_bwd": (_I, [_DESC, C.POINTER(ob_block_attn), C.POINTER(ob_block_weights), C.POINTER(ob_block_grads), _I, _P, _P, _P, _P,
+                               _Z, _SEG, _P, _Z, _P]),
+    "ob_varlen_attn_window_bwd_plan": (_I, [_SEG, _I, _I, _I, _I, _I, C.POINTER(ob_attn_bwd_launch), C.POINTER(C.c_int), C.POINTER(C.c_int)]),
     "ob_gemm_workspace_bytes": (_Z, [_I, _I, _I, _I]),
     "ob_gemm_bf16": (_I, [_I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "ob_gemm_plan": (_I, [_I, _I, _I, _I, _I, C.POINTER(ob_gemm_launch), C.POINTER(C.c_int)]),
@@ -303,6 +312,32 @@ def ob_block_bwd(desc, weights: dict, grads: dict, flags, x, dy, dx, saved,
                             _stream(stream)))
 
 
+class BlockAttn:
+    """What a block's attention does otherwise than its description says; holds the rotary description and positions alive."""
+
+    def __init__(self, window=0, sinks=0, rotary=None, pos=None):
+        self.rotary, self.pos = rotary, pos
+        self.c = ob_block_attn(int(window), int(sinks), None if rotary is None else C.pointer(rotary), _ptr(pos))
+
+
+def ob_block_attn_workspace_bytes(desc, attn: BlockAttn, seg: Segments) -> int:
+    return lib.ob_block_attn_workspace_bytes(C.byref(desc), C.byref(attn.c), C.byref(seg.c))
+
+
+def ob_block_attn_fwd(desc, attn: BlockAttn, weights: dict, x, y, saved, seg: Segments, ws, stream=None):
+    w = _weights_struct(ob_block_weights, weights)
+    _check(lib.ob_block_attn_fwd(C.byref(desc), C.byref(attn.c), C.byref(w), _ptr(x), _ptr(y), _ptr(saved), _nbytes(saved), C.byref(seg.c),
+                                 _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def ob_block_attn_bwd(desc, attn: BlockAttn, weights: dict, grads: dict, flags, x, dy, dx, saved, seg: Segments, ws, stream=None):
+    """flags: as ob_block_bwd"""
+    w = _weights_struct(ob_block_weights, weights)
+    g = _weights_struct(ob_block_grads, grads)
+    _check(lib.ob_block_attn_bwd(C.byref(desc), C.byref(attn.c), C.byref(w), C.byref(g), int(flags), _ptr(x), _ptr(dy), _ptr(dx),
+                                 _ptr(saved), _nbytes(saved), C.byref(seg.c), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
 def ob_gemm_workspace_bytes(layout, M, N, K) -> int:
     return lib.ob_gemm_workspace_bytes(layout, M, N, K)
 
@@ -349,6 +384,13 @@ def ob_varlen_attn_bwd_threads(seg, nq, nkv, d, mask) -> int:
     out = C.c_int()
     _check(lib.ob_varlen_attn_bwd_threads(C.byref(seg.c), nq, nkv, d, int(mask), C.byref(out)))
     return out.value
+
+
+def ob_varlen_attn_window_bwd_plan(seg: Segments, nq, nkv, d, window, sinks=0):
+    """(ob_attn_bwd_launch, threads of a workgroup, chunks of the sinks' sums)"""
+    out, threads, chunks = ob_attn_bwd_launch(), C.c_int(), C.c_int()
+    _check(lib.ob_varlen_attn_window_bwd_plan(C.byref(seg.c), nq, nkv, d, window, sinks, C.byref(out), C.byref(threads), C.byref(chunks)))
+    return out, threads.value, chunks.value
 
 
 class RowIndex:

@@ -317,7 +317,7 @@ static int validate_block(const ob_block_desc *desc, const ob_block_weights *w, 
 // of the re-computation path, which has no use for the block output).  A GEMM with an activation checks its launch, which clears the device's
 // last error: its status is this one's; the other launches are left to the caller's check.
 static int block_fwd_bf16(const ob_block_desc *desc, const ob_block_weights *w, const void *x, void *y,
-                          void *saved, const ob_segments *seg, hipStream_t s) {
+                          void *saved, const ob_segments *seg, hipStream_t s, const BlockSteps *steps) {
     const Dims m = dims_of(desc, seg->total_tokens);
     const Saved sv = saved_layout(m);
     const bool bias = desc->has_bias != 0;
@@ -330,9 +330,11 @@ static int block_fwd_bf16(const ob_block_desc *desc, const ob_block_weights *w, 
 
     launch_norm_fwd(desc->norm, x, w->n1_g, beta ? w->n1_b : nullptr, h1, (float *)at(saved, sv.stat1), m.T, m.H, desc->norm_eps, s);
     launch_gemm_nt(m.T, m.Dqkv, m.H, h1, m.H, w->w_qkv, m.H, qkv, m.Dqkv, bias ? w->b_qkv : nullptr, nullptr, 0, s, 0, gws);
-    if (desc->use_rotary)
+    if (steps && steps->rotate) steps->rotate(*steps, qkv, m.T, 0, s);
+    else if (desc->use_rotary)
         launch_rotary(qkv, m.Dqkv, m.T, m.nq + m.nkv, m.d, seg->cu_dev, seg->n_seg, desc->rotary_base, 1.0f, s);
-    launch_attn_fwd(qkv, qkv + (size_t)m.nq * m.d * 2, qkv + (size_t)(m.nq + m.nkv) * m.d * 2, o, lse, m.Dqkv,
+    if (steps && steps->attn_fwd) steps->attn_fwd(*steps, qkv, o, lse, seg, s);
+    else launch_attn_fwd(qkv, qkv + (size_t)m.nq * m.d * 2, qkv + (size_t)(m.nq + m.nkv) * m.d * 2, o, lse, m.Dqkv,
                     m.Dqkv, m.HD, seg, m.nq, m.nkv, m.d, scale, desc->mask, s);
     launch_gemm_nt(m.T, m.H, m.HD, o, m.HD, w->w_o, m.HD, x1, m.H, bias ? w->b_o : nullptr, x, m.H, s, 0, gws);
     launch_norm_fwd(desc->norm, x1, w->n2_g, beta ? w->n2_b : nullptr, h2, (float *)at(saved, sv.stat2), m.T, m.H, desc->norm_eps, s);
@@ -346,41 +348,50 @@ static int block_fwd_bf16(const ob_block_desc *desc, const ob_block_weights *w, 
     return OB_OK;
 }
 
+int ob::block_fwd(const char *who, const ob_block_desc *desc, const ob_block_weights *w, const void *x, void *y, void *saved,
+                  size_t saved_bytes, const ob_segments *seg, void *ws, size_t ws_bytes, hipStream_t s, const BlockSteps *steps) {
+    if (!x || !y) return fail(OB_EINVAL, "%s: x / y is null", who);
+    if (int rc = validate_block(desc, w, seg, saved, saved_bytes, ws, ws_bytes, who)) return rc;
+    if (desc->dtype == OB_FP32) {
+        if (steps) steps->f32_fwd(*steps, w, x, y, saved, seg, s);
+        else f32::block_fwd(desc, w, x, y, saved, seg, s);
+    } else if (int rc = block_fwd_bf16(desc, w, x, y, saved, seg, s, steps)) return rc;
+    return check_launch(who);
+}
+
 extern "C" int ob_block_fwd(const ob_block_desc *desc, const ob_block_weights *w, const void *x, void *y,
                             void *saved, size_t saved_bytes, const ob_segments *seg, void *ws,
                             size_t ws_bytes, void *hip_stream) {
-    if (!x || !y) return fail(OB_EINVAL, "ob_block_fwd: x / y is null");
-    if (int rc = validate_block(desc, w, seg, saved, saved_bytes, ws, ws_bytes, "ob_block_fwd")) return rc;
-    hipStream_t s = (hipStream_t)hip_stream;
-    if (desc->dtype == OB_FP32) f32::block_fwd(desc, w, x, y, saved, seg, s);
-    else if (int rc = block_fwd_bf16(desc, w, x, y, saved, seg, s)) return rc;
-    return check_launch("ob_block_fwd");
+    return block_fwd("ob_block_fwd", desc, w, x, y, saved, saved_bytes, seg, ws, ws_bytes, (hipStream_t)hip_stream, nullptr);
 }
 
-extern "C" int ob_block_bwd(const ob_block_desc *desc, const ob_block_weights *w, const ob_block_grads *g,
-                            int flags, const void *x, const void *dy, void *dx,
-                            void *saved, size_t saved_bytes, const ob_segments *seg, void *ws,
-                            size_t ws_bytes, void *hip_stream) {
-    if (!x || !dy || !dx) return fail(OB_EINVAL, "ob_block_bwd: x / dy / dx is null");
-    if (flags & ~(OB_BWD_ACCUMULATE | OB_BWD_RECOMPUTE)) return fail(OB_EINVAL, "ob_block_bwd: unknown flag bits %d", flags);
+int ob::block_bwd(const char *who, const ob_block_desc *desc, const ob_block_weights *w, const ob_block_grads *g, int flags, const void *x,
+                  const void *dy, void *dx, void *saved, size_t saved_bytes, const ob_segments *seg, void *ws, size_t ws_bytes,
+                  hipStream_t s, const BlockSteps *steps) {
+    if (!x || !dy || !dx) return fail(OB_EINVAL, "%s: x / dy / dx is null", who);
+    if (flags & ~(OB_BWD_ACCUMULATE | OB_BWD_RECOMPUTE)) return fail(OB_EINVAL, "%s: unknown flag bits %d", who, flags);
     const int accumulate_wgrad = flags & OB_BWD_ACCUMULATE;
-    if (int rc = validate_block(desc, w, seg, saved, saved_bytes, ws, ws_bytes, "ob_block_bwd")) return rc;
-    if (!g) return fail(OB_EINVAL, "ob_block_bwd: grads is null");
+    if (int rc = validate_block(desc, w, seg, saved, saved_bytes, ws, ws_bytes, who)) return rc;
+    if (!g) return fail(OB_EINVAL, "%s: grads is null", who);
     if (!g->n1_g || !g->w_qkv || !g->w_o || !g->n2_g || !g->w_up || !g->w_down)
-        return fail(OB_EINVAL, "ob_block_bwd: a required gradient pointer is null");
+        return fail(OB_EINVAL, "%s: a required gradient pointer is null", who);
     const bool bias = desc->has_bias != 0;
     const bool beta = bias && desc->norm == OB_LAYERNORM;
-    if (bias && (!g->b_qkv || !g->b_o || !g->b_up || !g->b_down)) return fail(OB_EINVAL, "ob_block_bwd: a bias gradient pointer is null");
-    if (beta && (!g->n1_b || !g->n2_b)) return fail(OB_EINVAL, "ob_block_bwd: a beta gradient pointer is null");
+    if (bias && (!g->b_qkv || !g->b_o || !g->b_up || !g->b_down)) return fail(OB_EINVAL, "%s: a bias gradient pointer is null", who);
+    if (beta && (!g->n1_b || !g->n2_b)) return fail(OB_EINVAL, "%s: a beta gradient pointer is null", who);
 
-    hipStream_t s = (hipStream_t)hip_stream;
     if (desc->dtype == OB_FP32) {
+        if (steps) {
+            if (flags & OB_BWD_RECOMPUTE) steps->f32_fwd(*steps, w, x, nullptr, saved, seg, s);
+            steps->f32_bwd(*steps, w, g, accumulate_wgrad ? 1 : 0, x, dy, dx, saved, seg, ws, s);
+            return check_launch(who);
+        }
         if (flags & OB_BWD_RECOMPUTE) f32::block_fwd(desc, w, x, nullptr, saved, seg, s);
         f32::block_bwd(desc, w, g, accumulate_wgrad ? 1 : 0, x, dy, dx, saved, seg, ws, s);
-        return check_launch("ob_block_bwd");
+        return check_launch(who);
     }
     if (flags & OB_BWD_RECOMPUTE)
-        if (int rc = block_fwd_bf16(desc, w, x, nullptr, saved, seg, s)) return rc;
+        if (int rc = block_fwd_bf16(desc, w, x, nullptr, saved, seg, s, steps)) return rc;
     const Dims m = dims_of(desc, seg->total_tokens);
     const Saved sv = saved_layout(m);
     const Work wk = work_layout(m);
@@ -440,11 +451,18 @@ extern "C" int ob_block_bwd(const ob_block_desc *desc, const ob_block_weights *w
     if ((rc = gemm_any(1, m.T, m.HD, m.H, dx1, w->w_o, d_o, nullptr, nullptr, gws, wk.gemm_bytes, s))) return rc;
     // attention
     float *lse2 = (float *)at(ws, wk.lse2);
-    // (the rotary backward of dq and dk happens in the attention kernels' epilogues)
-    launch_attn_bwd(d_o, qkv, qkv + (size_t)m.nq * m.d * 2, qkv + (size_t)(m.nq + m.nkv) * m.d * 2, o, lse, lse2, delta,
-                    dqkv, dqkv + (size_t)m.nq * m.d * 2, dqkv + (size_t)(m.nq + m.nkv) * m.d * 2,
-                    m.Dqkv, m.Dqkv, m.HD, seg, m.nq, m.nkv, m.d, scale, desc->mask,
-                    desc->use_rotary ? desc->rotary_base : 0.f, s);
+    // (the rotary backward of dq and dk happens in the attention kernels' epilogues, or behind steps of the block's own)
+    if (steps && steps->attn_bwd) {
+        steps->attn_bwd(*steps, d_o, qkv, o, lse, lse2, delta, dqkv, seg, s);
+        if (desc->use_rotary)
+            launch_rotary(dqkv, m.Dqkv, m.T, m.nq + m.nkv, m.d, seg->cu_dev, seg->n_seg, desc->rotary_base, -1.0f, s);
+    } else {
+        launch_attn_bwd(d_o, qkv, qkv + (size_t)m.nq * m.d * 2, qkv + (size_t)(m.nq + m.nkv) * m.d * 2, o, lse, lse2, delta,
+                        dqkv, dqkv + (size_t)m.nq * m.d * 2, dqkv + (size_t)(m.nq + m.nkv) * m.d * 2,
+                        m.Dqkv, m.Dqkv, m.HD, seg, m.nq, m.nkv, m.d, scale, desc->mask,
+                        desc->use_rotary ? desc->rotary_base : 0.f, s);
+    }
+    if (steps && steps->rotate) steps->rotate(*steps, dqkv, m.T, 1, s);
     // qkv = h1 W_qkv^T + b_qkv
     if (bias) bias_grad(dqkv, m.Dqkv, wk.p_qkv, g->b_qkv);
     if ((rc = gemm_any(1, m.T, m.H, m.Dqkv, dqkv, w->w_qkv, dh, nullptr, nullptr, gws, wk.gemm_bytes, s))) return rc;
@@ -460,7 +478,14 @@ extern "C" int ob_block_bwd(const ob_block_desc *desc, const ob_block_weights *w
                               {m.Dqkv, m.H, dqkv, h1, g->w_qkv, acc ? g->w_qkv : nullptr}};
     if ((rc = gemm_tn_group(4, wgrads, m.T, gws, wk.gemm_bytes, s))) return rc;
     if ((rc = launch_reduce_batch(sums, acc, s))) return rc;
-    return check_launch("ob_block_bwd");
+    return check_launch(who);
+}
+
+extern "C" int ob_block_bwd(const ob_block_desc *desc, const ob_block_weights *w, const ob_block_grads *g,
+                            int flags, const void *x, const void *dy, void *dx,
+                            void *saved, size_t saved_bytes, const ob_segments *seg, void *ws,
+                            size_t ws_bytes, void *hip_stream) {
+    return block_bwd("ob_block_bwd", desc, w, g, flags, x, dy, dx, saved, saved_bytes, seg, ws, ws_bytes, (hipStream_t)hip_stream, nullptr);
 }
 
 extern "C" size_t ob_gemm_workspace_bytes(int layout, int M, int N, int K) {

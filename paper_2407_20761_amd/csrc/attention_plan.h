@@ -52,6 +52,7 @@ __host__ __device__ constexpr uint32_t dkv_piece_offset(uint32_t voff, uint32_t 
 int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window = 0, int whole = 0);
 int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal, int window = 0, int whole = 0);
 
+constexpr int MAX_SINKS = 64;      // they lie in a segment's first tile of keys
 // The sinks of a segment are seen by all of its rows.  Up to sink_whole_rows() the workgroup of its first keys walks them all: what that adds to its
 // walk, rows past the window times the heads of a group, is to cost less than the two launches of the other way (about 25 trips of 64 rows).
 // Beyond, chunks of SINK_CHUNK rows leave fp32 sums.  Both are the segment's own, so that it gives the same sums in every batch.

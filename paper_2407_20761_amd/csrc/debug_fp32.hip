@@ -466,8 +466,8 @@ WorkF32 work_layout(const ob_block_desc *dsc, int T_) {
 #define OB_F(p) ((const float *)(p))
 #define OB_FM(p) ((float *)(p))
 
-void block_fwd(const ob_block_desc *dsc, const ob_block_weights *w, const void *x, void *y, void *saved,
-               const ob_segments *seg, hipStream_t s) {
+static void run_block_fwd(const ob_block_desc *dsc, const ob_block_weights *w, const void *x, void *y, void *saved,
+                          const ob_segments *seg, hipStream_t s, const BlockSteps *st) {
     const int T = seg->total_tokens, H = dsc->hidden, d = dsc->head_dim, nq = dsc->n_q_heads, nkv = dsc->n_kv_heads;
     const int F = dsc->mlp_dim, upF = dsc->mlp == OB_SWIGLU ? 2 * F : F, Dq = (nq + 2 * nkv) * d, HD = nq * d;
     const SavedF32 sv = saved_layout(dsc, T);
@@ -479,10 +479,12 @@ void block_fwd(const ob_block_desc *dsc, const ob_block_weights *w, const void *
     hipLaunchKernelGGL(norm_fwd_kernel, dim3(T), dim3(256), 0, s, ln ? 1 : 0, OB_F(x), OB_F(w->n1_g),
                        beta ? OB_F(w->n1_b) : nullptr, h1, OB_FM(b + sv.stat1), H, dsc->norm_eps);
     gemm(0, T, Dq, H, h1, OB_F(w->w_qkv), qkv, bias ? OB_F(w->b_qkv) : nullptr, nullptr, 0, s);
-    if (dsc->use_rotary)
+    if (st && st->rotate) st->rotate(*st, qkv, T, 0, s);
+    else if (dsc->use_rotary)
         hipLaunchKernelGGL(rotary_kernel, dim3(blocks_for((long)T * (nq + nkv) * (d / 2))), dim3(256), 0, s, qkv, Dq, T,
                            nq + nkv, d, seg->cu_dev, seg->n_seg, dsc->rotary_base, 1.0f);
-    attn_fwd(qkv, qkv + HD, qkv + HD + nkv * d, o, lse, Dq, Dq, HD, seg, nq, nkv, d, scale, dsc->mask, s);
+    if (st && st->window) attn_window_fwd(qkv, qkv + HD, qkv + HD + nkv * d, o, lse, Dq, Dq, HD, seg, nq, nkv, d, scale, st->window, st->sinks, s);
+    else attn_fwd(qkv, qkv + HD, qkv + HD + nkv * d, o, lse, Dq, Dq, HD, seg, nq, nkv, d, scale, dsc->mask, s);
     gemm(0, T, H, HD, o, OB_F(w->w_o), x1, bias ? OB_F(w->b_o) : nullptr, OB_F(x), 0, s);
     hipLaunchKernelGGL(norm_fwd_kernel, dim3(T), dim3(256), 0, s, ln ? 1 : 0, x1, OB_F(w->n2_g),
                        beta ? OB_F(w->n2_b) : nullptr, h2, OB_FM(b + sv.stat2), H, dsc->norm_eps);
@@ -492,8 +494,9 @@ void block_fwd(const ob_block_desc *dsc, const ob_block_weights *w, const void *
     if (y) gemm(0, T, H, F, act, OB_F(w->w_down), OB_FM(y), bias ? OB_F(w->b_down) : nullptr, x1, 0, s);
 }
 
-void block_bwd(const ob_block_desc *dsc, const ob_block_weights *w, const ob_block_grads *g, int acc, const void *x,
-               const void *dy, void *dx, const void *saved, const ob_segments *seg, void *ws, hipStream_t s) {
+static void run_block_bwd(const ob_block_desc *dsc, const ob_block_weights *w, const ob_block_grads *g, int acc, const void *x,
+                          const void *dy, void *dx, const void *saved, const ob_segments *seg, void *ws, hipStream_t s,
+                          const BlockSteps *st) {
     const int T = seg->total_tokens, H = dsc->hidden, d = dsc->head_dim, nq = dsc->n_q_heads, nkv = dsc->n_kv_heads;
     const int F = dsc->mlp_dim, upF = dsc->mlp == OB_SWIGLU ? 2 * F : F, Dq = (nq + 2 * nkv) * d, HD = nq * d;
     const SavedF32 sv = saved_layout(dsc, T);
@@ -527,9 +530,14 @@ void block_bwd(const ob_block_desc *dsc, const ob_block_weights *w, const ob_blo
     gemm(2, H, HD, T, dx1, o, OB_FM(g->w_o), nullptr, nullptr, acc, s);
     if (bias) colsum(dx1, H, g->b_o);
     gemm(1, T, HD, H, dx1, OB_F(w->w_o), d_o, nullptr, nullptr, 0, s);
-    attn_bwd(d_o, qkv, qkv + HD, qkv + HD + nkv * d, o, lse, dqkv, dqkv + HD, dqkv + HD + nkv * d, delta, Dq, Dq, HD,
-             seg, nq, nkv, d, scale, dsc->mask, s);
-    if (dsc->use_rotary)
+    if (st && st->window)
+        attn_window_bwd(d_o, qkv, qkv + HD, qkv + HD + nkv * d, o, lse, dqkv, dqkv + HD, dqkv + HD + nkv * d, delta, Dq, Dq, HD, seg, nq, nkv, d,
+                        scale, st->window, st->sinks, s);
+    else
+        attn_bwd(d_o, qkv, qkv + HD, qkv + HD + nkv * d, o, lse, dqkv, dqkv + HD, dqkv + HD + nkv * d, delta, Dq, Dq, HD,
+                 seg, nq, nkv, d, scale, dsc->mask, s);
+    if (st && st->rotate) st->rotate(*st, dqkv, T, 1, s);
+    else if (dsc->use_rotary)
         hipLaunchKernelGGL(rotary_kernel, dim3(blocks_for((long)T * (nq + nkv) * (d / 2))), dim3(256), 0, s, dqkv, Dq, T,
                            nq + nkv, d, seg->cu_dev, seg->n_seg, dsc->rotary_base, -1.0f);
     // qkv = h1 W_qkv^T + b_qkv
@@ -543,6 +551,23 @@ void block_bwd(const ob_block_desc *dsc, const ob_block_weights *w, const ob_blo
                        OB_FM(g->n1_g), beta ? OB_FM(g->n1_b) : nullptr, T, H, acc);
 }
 
+
+void block_fwd(const ob_block_desc *dsc, const ob_block_weights *w, const void *x, void *y, void *saved,
+               const ob_segments *seg, hipStream_t s) {
+    run_block_fwd(dsc, w, x, y, saved, seg, s, nullptr);
+}
+void block_bwd(const ob_block_desc *dsc, const ob_block_weights *w, const ob_block_grads *g, int acc, const void *x,
+               const void *dy, void *dx, const void *saved, const ob_segments *seg, void *ws, hipStream_t s) {
+    run_block_bwd(dsc, w, g, acc, x, dy, dx, saved, seg, ws, s, nullptr);
+}
+void block_steps_fwd(const BlockSteps &st, const ob_block_weights *w, const void *x, void *y, void *saved, const ob_segments *seg,
+                     hipStream_t s) {
+    run_block_fwd(st.desc, w, x, y, saved, seg, s, &st);
+}
+void block_steps_bwd(const BlockSteps &st, const ob_block_weights *w, const ob_block_grads *g, int acc, const void *x, const void *dy,
+                     void *dx, const void *saved, const ob_segments *seg, void *ws, hipStream_t s) {
+    run_block_bwd(st.desc, w, g, acc, x, dy, dx, saved, seg, ws, s, &st);
+}
 
 // ---- hand-over, fp32: the same steps as the bf16 path, every tensor in fp32, u kept in `saved` ----
 struct ConnSaved { size_t u, un, h, a, stats, total; };

@@ -159,6 +159,30 @@ int rotary_table(const ob_rotary_axes_desc *desc, RotaryTable &table, const char
 void launch_rotary_axes(const void *x, int ldx, void *y, int ldy, int T, int n_heads, int d, const RotaryTable &table,
                         const int32_t *pos, int inverse, int dtype, hipStream_t s);
 
+// ---- one transformer block (api.cpp) ---------------------------------------------------------------
+// What a block does otherwise than its description says (block_attn_api.cpp): the rotary positions, the attention.  Null members: as described.
+struct BlockSteps {
+    const ob_block_desc *desc;
+    RotaryTable table;
+    const int32_t *pos;
+    int window, sinks;
+    float *part;          // launch_attn_window_bwd()
+    // the query and key heads of qkv, or of its gradient (inverse), in place
+    void (*rotate)(const BlockSteps &st, void *qkv, int T, int inverse, hipStream_t s);
+    void (*attn_fwd)(const BlockSteps &st, const void *qkv, void *o, float *lse, const ob_segments *seg, hipStream_t s);
+    void (*attn_bwd)(const BlockSteps &st, const void *d_o, const void *qkv, const void *o, const float *lse, float *lse2, float *delta,
+                     void *dqkv, const ob_segments *seg, hipStream_t s);
+    // the whole block in fp32
+    void (*f32_fwd)(const BlockSteps &st, const ob_block_weights *w, const void *x, void *y, void *saved, const ob_segments *seg, hipStream_t s);
+    void (*f32_bwd)(const BlockSteps &st, const ob_block_weights *w, const ob_block_grads *g, int accumulate, const void *x, const void *dy,
+                    void *dx, const void *saved, const ob_segments *seg, void *ws, hipStream_t s);
+};
+int block_fwd(const char *who, const ob_block_desc *desc, const ob_block_weights *w, const void *x, void *y, void *saved,
+              size_t saved_bytes, const ob_segments *seg, void *ws, size_t ws_bytes, hipStream_t s, const BlockSteps *steps);
+int block_bwd(const char *who, const ob_block_desc *desc, const ob_block_weights *w, const ob_block_grads *g, int flags, const void *x,
+              const void *dy, void *dx, void *saved, size_t saved_bytes, const ob_segments *seg, void *ws, size_t ws_bytes, hipStream_t s,
+              const BlockSteps *steps);
+
 // ---- fp32 debug path (debug_fp32.hip): every tensor fp32, plain FMA kernels --------------------
 namespace f32 {
 struct SavedF32 { size_t h1, qkv, o, lse, x1, h2, up, act, stat1, stat2, total; };
@@ -181,6 +205,9 @@ void block_fwd(const ob_block_desc *dsc, const ob_block_weights *w, const void *
 void block_bwd(const ob_block_desc *dsc, const ob_block_weights *w, const ob_block_grads *g, int accumulate,
                const void *x, const void *dy, void *dx, const void *saved, const ob_segments *seg, void *ws,
                hipStream_t s);
+void block_steps_fwd(const BlockSteps &st, const ob_block_weights *w, const void *x, void *y, void *saved, const ob_segments *seg, hipStream_t s);
+void block_steps_bwd(const BlockSteps &st, const ob_block_weights *w, const ob_block_grads *g, int accumulate, const void *x, const void *dy,
+                     void *dx, const void *saved, const ob_segments *seg, void *ws, hipStream_t s);
 // the cross entropy with every tensor in fp32, a few rows of logits at a time; rows_dev may be null (all of them)
 size_t lm_loss_work_bytes(int n, int H, int V);
 void lm_loss_fwd(const void *w, const void *x, const int32_t *rows_dev, int n, int H, int V, const int32_t *labels, float *nll, float *lse,

@@ -8,7 +8,6 @@ using namespace ob;
 
 namespace {
 
-constexpr int MAX_SINKS = 64;           // they lie in a segment's first tile of keys
 constexpr int MAX_STRIDE = 1 << 24;     // elements: the offsets inside a tile of 64 rows have 32 bits
 
 // `window` is cut to the longest segment there may be
@@ -74,4 +73,19 @@ extern "C" int ob_varlen_attn_window_bwd(const void *d_o, const void *q, const v
         launch_attn_window_bwd(d_o, q, k, v, o, lse, (float *)(at + w.lse2), (float *)(at + w.delta), (float *)(at + w.part), dq, dk, dv, ldq,
                                ldkv, ldo, seg, nq, nkv, d, scale, window, sinks, s);
     return check_launch(who);
+}
+
+extern "C" int ob_varlen_attn_window_bwd_plan(const ob_segments *seg, int nq, int nkv, int d, int window, int sinks,
+                                              ob_attn_bwd_launch *launch, int *threads, int *chunks) {
+    const char *who = "ob_varlen_attn_window_bwd_plan";
+    if (!launch || !threads || !chunks) return fail(OB_EINVAL, "%s: null output", who);
+    if (int rc = validate(seg, nq, nkv, d, nq * d, nkv * d, nq * d, 1.f, &window, sinks, OB_BF16, who)) return rc;
+    const int whole = sinks ? sink_whole_rows(window, nq / nkv) : 0, shape = dkv_shape(seg, nkv, nq / nkv, d, true, window, whole);
+    const int key_rows = 32 * dkv_np(d, shape);
+    TileOrder ord;
+    const int places = make_order(seg, key_rows, true, true, ord, window, whole);
+    *launch = ob_attn_bwd_launch{key_rows, dkv_sr(d, shape), places, ord.n ? key_rows << ord.unit_log2 : 0};
+    *threads = dkv_threads(d, shape);
+    *chunks = sink_chunks(seg, whole, sinks);
+    return OB_OK;
 }

@@ -1,0 +1,279 @@
+"""The language-model side of a training step run as one: blocks with rotary positions of several axes, a window and sinks, the loss at their end,
+and back through both, against the oracle's block with these steps in 64 bits."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2407_20761_amd as ob
+import synth_inputs as si
+from conftest import rel_err
+from gpu_util import bytes_buf, to_dev, to_np
+from oracle import block as orc
+from window_ref import allowed
+
+gpu = pytest.mark.gpu
+DEV = "cuda"
+# (the framework's bars: fp32 storage 1e-4, bf16 storage 2e-2 of a tensor's largest value, as in every block test)
+TOL = {torch.float32: 1e-4, torch.bfloat16: 2e-2}
+
+
+def _shape(**kw):
+    base = dict(hidden=256, n_q_heads=4, n_kv_heads=2, head_dim=64, mlp_dim=320, norm=si.NORM_RMSNORM, mlp=si.MLP_SWIGLU, mask=si.MASK_CAUSAL,
+                use_rotary=False, has_bias=False, norm_eps=1e-6)
+    base.update(kw)
+    return si.small_shape(**base)
+
+
+def _positions(cu, axes, seed):
+    """a grid of visual tokens at every sample's start, text counting on behind it"""
+    rng, rows = np.random.default_rng(seed), []
+    for a, b in zip(cu[:-1], cu[1:]):
+        n = b - a
+        seen = int(rng.integers(0, n + 1))
+        j = np.arange(seen)
+        p = np.stack([0 * j, j // 8, j % 8])[:axes]
+        text = np.broadcast_to(9 + np.arange(n - seen), (axes, n - seen))
+        rows.append(np.concatenate([p, text], 1))
+    return np.concatenate(rows, 1).astype(np.int32)
+
+
+class Attn:
+    """window, sinks and axes of a run, on the device and as the oracle's block sees them"""
+
+    def __init__(self, shape, cu, window, sinks, axes=(0, 1, 2), base=1000.0, seed=0):
+        self.cu, self.window, self.sinks, self.base = cu, window, sinks, base
+        self.pair_axes = [axes[i % len(axes)] for i in range(shape.head_dim // 2)] if axes else None
+        pos = _positions(cu, 3, seed)
+        self.pos_host, self.pos = pos, torch.from_numpy(pos).to(DEV)
+        rotary = ob.make_rotary_axes_desc(self.pair_axes, shape.head_dim, base) if axes else None
+        self.c = ob.BlockAttn(window, sinks, rotary, self.pos if axes else None)
+
+    def patch(self, monkeypatch):
+        def mask(cu, T, kind):
+            out = np.zeros((T, T), dtype=bool)
+            for a, b in zip(cu[:-1], cu[1:]):
+                out[a:b, a:b] = allowed(b - a, self.window or b - a, self.sinks)
+            return out
+
+        def angles(cu, T, d, base, dtype=np.float64):
+            theta = np.float64(np.float32(self.base)) ** (-2.0 * np.arange(d // 2) / d)
+            return np.stack([self.pos_host[a] * theta[i] if a >= 0 else 0.0 * self.pos_host[0] for i, a in enumerate(self.pair_axes)], 1).astype(dtype)
+        monkeypatch.setattr(orc, "allowed_mask", mask)
+        if self.pair_axes:
+            monkeypatch.setattr(orc, "rotary_angles", angles)
+
+
+class Block:
+    def __init__(self, shape, cu, attn, dtype, seed):
+        self.shape, self.attn, self.seg, T = shape, attn, ob.Segments(np.asarray(cu, dtype=np.int32)), int(cu[-1])
+        self.desc = ob.make_desc(shape, ob.OB_BF16 if dtype == torch.bfloat16 else ob.OB_FP32)
+        self.w_np = si.block_weights(shape, seed=seed)
+        self.w = {n: to_dev(a, dtype) for n, a in self.w_np.items()}
+        self.g = {n: torch.full_like(t, float("nan")) for n, t in self.w.items()}
+        self.saved = bytes_buf(ob.ob_block_saved_bytes(self.desc, T))
+        n = ob.ob_block_attn_workspace_bytes(self.desc, attn.c, self.seg)
+        assert n >= ob.ob_block_workspace_bytes(self.desc, T) > 0
+        self.ws = torch.full((n,), 255, dtype=torch.uint8, device=DEV)
+
+    def fwd(self, x):
+        y = torch.full_like(x, float("nan"))
+        ob.ob_block_attn_fwd(self.desc, self.attn.c, self.w, x, y, self.saved, self.seg, self.ws)
+        return y
+
+    def bwd(self, x, dy, flags=0):
+        dx = torch.full_like(x, float("nan"))
+        ob.ob_block_attn_bwd(self.desc, self.attn.c, self.w, self.g, flags, x, dy, dx, self.saved, self.seg, self.ws)
+        return dx
+
+    def oracle_shape(self):
+        """(use_rotary: the patched angles)"""
+        return si.small_shape(**{**self.shape.__dict__, "use_rotary": self.shape.use_rotary or bool(self.attn.pair_axes)})
+
+
+def _compare(tol, got, want):
+    for n, ref in want.items():
+        e = rel_err(got[n], ref)
+        assert e < tol, (n, e)
+
+
+CASES = [
+    (dict(), [40, 1, 300, 129], 33, 4, (0, 1, 2)),
+    (dict(head_dim=128, n_q_heads=2, n_kv_heads=1), [200, 65], 64, 1, (0, 2, -1, 1)),
+    (dict(has_bias=True, norm=si.NORM_LAYERNORM, mlp=si.MLP_GELU, n_kv_heads=4), [130, 77], 50, 0, (1,)),
+    (dict(use_rotary=True, rotary_base=500.0), [90, 150], 20, 2, ()),           # the description's rotary behind a windowed attention
+    (dict(), [64, 90], 0, 0, (0, 1, 2)),                                       # axes alone
+    (dict(n_q_heads=8, n_kv_heads=1), [1700], 100, 16, (0, 1, 2)),             # sinks in chunks
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kw,lens,window,sinks,axes", CASES)
+def test_block(kw, lens, window, sinks, axes, dtype, monkeypatch):
+    print(f"block with attention steps: {kw} {lens} window={window} sinks={sinks} axes={axes} {dtype}", flush=True)
+    shape, cu = _shape(**kw), si.lengths_to_cu(lens)
+    attn = Attn(shape, cu, window, sinks, axes)
+    b = Block(shape, cu, attn, dtype, 1)
+    x_np, dy_np = si.activations(int(cu[-1]), shape.hidden, seed=2)
+    x, dy = to_dev(x_np, dtype), to_dev(dy_np, dtype)
+    y, dx = b.fwd(x), b.bwd(x, dy)
+    attn.patch(monkeypatch)
+    y_ref, cache = orc.block_fwd(b.oracle_shape(), b.w_np, x_np, cu)
+    dx_ref, g_ref, _ = orc.block_bwd(b.oracle_shape(), b.w_np, cache, dy_np, cu)
+    _compare(TOL[dtype], {"y": to_np(y), "dx": to_np(dx), **{n: to_np(t) for n, t in b.g.items()}}, {"y": y_ref, "dx": dx_ref, **g_ref})
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_recomputation_and_accumulation(dtype):
+    shape, cu = _shape(), si.lengths_to_cu([300, 140])
+    b = Block(shape, cu, Attn(shape, cu, 60, 4), dtype, 3)
+    x, dy = (to_dev(a, dtype) for a in si.activations(int(cu[-1]), shape.hidden, seed=4))
+    b.fwd(x)
+    dx = b.bwd(x, dy)
+    first = {n: t.clone() for n, t in b.g.items()}
+    b.saved.fill_(255)
+    assert torch.equal(b.bwd(x, dy, ob.OB_BWD_RECOMPUTE), dx)
+    assert all(torch.equal(b.g[n], first[n]) for n in first)
+    b.bwd(x, dy, ob.OB_BWD_ACCUMULATE)
+    for n, t in b.g.items():          # twice the gradient: exact but for one rounding of the sum
+        assert float((t.double() - 2 * first[n].double()).abs().max()) <= 2 * torch.finfo(dtype).eps * float(first[n].double().abs().max()), n
+
+
+@gpu
+def test_no_step_at_all_is_the_plain_block():
+    shape, cu = _shape(use_rotary=True), si.lengths_to_cu([200, 57])
+    b = Block(shape, cu, Attn(shape, cu, 0, 0, ()), torch.bfloat16, 5)
+    x, dy = (to_dev(a) for a in si.activations(int(cu[-1]), shape.hidden, seed=6))
+    y, dx = b.fwd(x), b.bwd(x, dy)
+    y2, dx2, g2 = torch.empty_like(y), torch.empty_like(dx), {n: torch.empty_like(t) for n, t in b.g.items()}
+    ob.ob_block_fwd(b.desc, b.w, x, y2, b.saved, b.seg, b.ws)
+    ob.ob_block_bwd(b.desc, b.w, g2, 0, x, dy, dx2, b.saved, b.seg, b.ws)
+    assert torch.equal(y, y2) and torch.equal(dx, dx2) and all(torch.equal(b.g[n], g2[n]) for n in g2)
+
+
+class Step:
+    """two blocks and the loss over the supervised rows: one training step's forward and backward"""
+
+    def __init__(self, dtype, lens=(150, 1, 400), vocab=1009, window=70, sinks=4):
+        self.shape, self.cu, self.dtype = _shape(), si.lengths_to_cu(list(lens)), dtype
+        T, H = int(self.cu[-1]), self.shape.hidden
+        self.attn = Attn(self.shape, self.cu, window, sinks)
+        self.blocks = [Block(self.shape, self.cu, self.attn, dtype, 10 + i) for i in range(2)]
+        rng = np.random.default_rng(7)
+        self.x_np = si.activations(T, H, seed=8)[0]
+        self.w_np = si.round_to_bf16((rng.standard_normal((vocab, H)) * 0.1).astype(np.float32))
+        self.rows_np = np.sort(rng.permutation(T)[:T // 3]).astype(np.int32)
+        n = len(self.rows_np)
+        self.labels_np = rng.integers(0, vocab, n).astype(np.int32)
+        self.labels_np[::9] = -100
+        self.dnll_np = np.full(n, 1.0 / n, dtype=np.float32)
+        self.x, self.w = to_dev(self.x_np, dtype), to_dev(self.w_np, dtype)
+        self.rows, self.labels, self.dnll = ob.RowIndex(self.rows_np), torch.from_numpy(self.labels_np).to(DEV), torch.from_numpy(self.dnll_np).to(DEV)
+        self.desc = ob.make_lm_loss_desc(H, vocab, ob.OB_BF16 if dtype == torch.bfloat16 else ob.OB_FP32)
+        self.ws = bytes_buf(ob.ob_lm_loss_workspace_bytes(self.desc, n))
+        self.nll, self.lse = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+        self.dw, self.dh = torch.empty_like(self.w), torch.empty_like(self.x)
+
+    def run(self):
+        T = self.x.shape[0]
+        h = [self.x]
+        for b in self.blocks:
+            h.append(b.fwd(h[-1]))
+        ob.ob_lm_loss_fwd(self.desc, self.w, h[-1], T, self.rows, self.labels, self.nll, self.lse, self.ws)
+        ob.ob_lm_loss_bwd(self.desc, 0, self.w, h[-1], T, self.rows, self.labels, self.lse, self.dnll, self.dh, self.dw, self.ws)
+        d = self.dh
+        for b, x in reversed(list(zip(self.blocks, h))):
+            d = b.bwd(x, d)
+        return {"nll": self.nll, "dw": self.dw, "dx": d, **{f"{i}.{n}": t for i, b in enumerate(self.blocks) for n, t in b.g.items()}}
+
+    def oracle(self):
+        h, caches = self.x_np.astype(np.float64), []
+        for b in self.blocks:
+            h, c = orc.block_fwd(b.oracle_shape(), b.w_np, h, self.cu)
+            caches.append(c)
+        z = h[self.rows_np] @ self.w_np.astype(np.float64).T
+        top = z.max(1, keepdims=True)
+        lse = top + np.log(np.exp(z - top).sum(1, keepdims=True))
+        has = (self.labels_np >= 0)[:, None]
+        hot = np.zeros_like(z)
+        hot[np.arange(len(z)), np.maximum(self.labels_np, 0)] = 1
+        G = np.where(has, np.exp(z - lse) - hot, 0) * self.dnll_np[:, None]
+        out = {"nll": np.where(has, lse - (z * hot).sum(1, keepdims=True), 0)[:, 0], "dw": G.T @ h[self.rows_np]}
+        d = np.zeros_like(h)
+        d[self.rows_np] = G @ self.w_np.astype(np.float64)
+        for i in (1, 0):
+            d, g, _ = orc.block_bwd(self.blocks[i].oracle_shape(), self.blocks[i].w_np, caches[i], d, self.cu)
+            out.update({f"{i}.{n}": t for n, t in g.items()})
+        return {**out, "dx": d}
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_training_step(dtype, monkeypatch):
+    s = Step(dtype)
+    got = {n: to_np(t) for n, t in s.run().items()}
+    s.attn.patch(monkeypatch)
+    _compare(TOL[dtype], got, s.oracle())
+
+
+@gpu
+def test_training_step_captured():
+    s = Step(torch.bfloat16)
+    want = {n: t.clone() for n, t in s.run().items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = s.run()
+    for _ in range(3):
+        for t in out.values():
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[n], want[n]) for n in want)
+        s.run()
+
+
+# ---- refusals: no GPU ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("status,text,desc_kw,kw", [
+    (1, "must not be negative", {}, {"window": -1}), (1, "must not be negative", {}, {"window": 5, "sinks": -2}), (3, "at most 64", {}, {"window": 5, "sinks": 65}),
+    (1, "causal", {"mask": si.MASK_BIDIR}, {"window": 5}), (1, "without a window", {}, {"sinks": 3}),
+    (1, "use_rotary", {"use_rotary": True}, {"rotary": 64}), (1, "heads of 128", {}, {"rotary": 128}), (1, "pos", {}, {"rotary": 64, "pos": None}),
+])
+def test_refusals(status, text, desc_kw, kw):
+    desc = ob.make_desc(_shape(**desc_kw))
+    rotary = ob.make_rotary_axes_desc([0] * (kw["rotary"] // 2), kw["rotary"]) if "rotary" in kw else None
+    attn = ob.ob_block_attn(kw.get("window", 0), kw.get("sinks", 0), None if rotary is None else C.pointer(rotary),
+                            kw.get("pos", 0x1000) if rotary is not None else None)
+    seg = ob.Segments(np.array([0, 10], dtype=np.int32), device=None)
+    seg.c.cu_dev = 0x1000
+    p = C.c_void_p(0x1000)
+    w = ob.ob_block_weights(*[0x1000] * 12)
+    g = ob.ob_block_grads(*[0x1000] * 12)
+    big = 1 << 40
+    assert ob.lib.ob_block_attn_workspace_bytes(C.byref(desc), C.byref(attn), C.byref(seg.c)) == 0
+    st = ob.lib.ob_block_attn_fwd(C.byref(desc), C.byref(attn), C.byref(w), p, p, p, big, C.byref(seg.c), p, big, None)
+    assert st == status and text in ob.ob_last_error(), ob.ob_last_error()
+    st = ob.lib.ob_block_attn_bwd(C.byref(desc), C.byref(attn), C.byref(w), C.byref(g), 0, p, p, p, p, big, C.byref(seg.c), p, big, None)
+    assert st == status and text in ob.ob_last_error(), ob.ob_last_error()
+
+
+def test_workspace_and_the_blocks_own_refusals():
+    desc = ob.make_desc(_shape(n_q_heads=2, n_kv_heads=1))
+    seg = ob.Segments(np.array([0, 2000], dtype=np.int32), device=None)
+    seg.c.cu_dev = 0x1000
+    plain, windowed = ob.BlockAttn(), ob.BlockAttn(100, 4)
+    own = ob.ob_block_workspace_bytes(desc, 2000)
+    assert ob.ob_block_attn_workspace_bytes(desc, plain, seg) == own
+    need = ob.ob_block_attn_workspace_bytes(desc, windowed, seg)
+    assert need == own + 8 * 2 * 4 * 64 * 4              # eight chunks of 256 rows, one key/value head
+    w, g, p = ob.ob_block_weights(*[0x1000] * 12), ob.ob_block_grads(*[0x1000] * 12), C.c_void_p(0x1000)
+    call = lambda d, s, n, ws: ob.lib.ob_block_attn_bwd(d, C.byref(windowed.c), C.byref(w), C.byref(g), 0, p, p, p, p, 1 << 40, s, ws, n, None)
+    assert call(C.byref(desc), C.byref(seg.c), need - 1, p) == ob.OB_EWORKSPACE
+    assert call(C.byref(desc), C.byref(seg.c), need, None) == ob.OB_EWORKSPACE
+    assert call(None, C.byref(seg.c), need, p) == ob.OB_EINVAL
+    assert call(C.byref(desc), None, need, p) == ob.OB_EINVAL
+    bad = ob.make_desc(_shape(hidden=100))
+    assert call(C.byref(bad), C.byref(seg.c), need, p) == ob.OB_EUNSUPPORTED

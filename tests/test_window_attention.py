@@ -279,3 +279,43 @@ def _host_segments(lens):
     s = ob.Segments(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32), device=None)
     s.c.cu_dev = 0x1000
     return s
+
+
+def _plan(lens, *a):
+    launch, threads, chunks = ob.ob_varlen_attn_window_bwd_plan(_host_segments(lens), *a)
+    return launch.key_rows, launch.query_rows, threads, chunks
+
+
+# every kernel of dK / dV has cases in test_forward_and_backward: (its case) -> key rows, query rows, threads, chunks of the sinks
+REACHED = [
+    (([1100], 2, 1, 64, 200, 3), (64, 64, 256, 5)), (([1500, 257], 4, 1, 64, 513, 16), (64, 64, 256, 6)),
+    (([1100], 2, 1, 128, 200, 3), (64, 64, 512, 5)), (([2101], 1, 1, 128, 700, 8), (64, 64, 512, 0)),
+    (([900], 6, 1, 128, 447, 64), (64, 64, 512, 4)),
+    # a full chip
+    (([2000] * 4, 16, 8, 64, 600, 4), (64, 32, 256, 32)), (([2000] * 4, 16, 8, 128, 600, 4), (128, 64, 512, 32)),
+    (([1100] * 4, 16, 8, 128, 600, 4), (64, 64, 512, 0)),
+]
+
+
+@pytest.mark.parametrize("case,want", REACHED)
+def test_which_kernel_a_case_reaches(case, want):
+    lens, nq, nkv, d, window, sinks = case
+    assert _plan(lens, nq, nkv, d, window, sinks) == want
+
+
+@gpu
+@pytest.mark.parametrize("lens,nq,nkv,d,window,sinks", [c for c, _ in REACHED[5:]])
+def test_full_chip(lens, nq, nkv, d, window, sinks):
+    _call(lens, nq, nkv, d, window, sinks).run().check()
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_launch_shapes_give_the_same_bits(d):
+    """a segment alone and among enough others to fill the chip, in another shape of dK / dV"""
+    lens, nq, nkv, window, sinks = [700, 333, 1290] + [2000] * 5, 16, 8, 600, 20
+    assert _plan(lens, nq, nkv, d, window, sinks)[:3] != _plan(lens[:1], nq, nkv, d, window, sinks)[:3]
+    c = _call(lens, nq, nkv, d, window, sinks).run()
+    for a, n in zip(np.concatenate([[0], np.cumsum(lens)])[:3], lens[:3]):
+        one = Call(c.qkv[a:a + n].clone(), c.d_o[a:a + n].clone(), [0, n], nq, nkv, d, window, sinks).run()
+        assert torch.equal(one.dqkv[:, :-16], c.dqkv[a:a + n, :-16])
