@@ -1210,7 +1210,7 @@ struct BandRows<Band> {
 };
 
 template <int D, bool CAUSAL, int NP, int SR, bool APART = false, class WIN = Whole>
-__global__ __launch_bounds__(128 * NP, D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 2) void attn_bwd_dkv_kernel(
+__global__ __launch_bounds__(128 * NP, D == 128 && SR == 32 ? 2 : D == 128 || NP == 6 ? 1 : SR == 32 ? 4 : 2) void attn_bwd_dkv_kernel(
     const __bf16 *__restrict__ d_o, const __bf16 *__restrict__ q, const __bf16 *__restrict__ k,
     const __bf16 *__restrict__ v, const float *__restrict__ lse2_all, const float *__restrict__ delta,
     __bf16 *__restrict__ dk, __bf16 *__restrict__ dv, int ldq, int ldkv, int ldo,
@@ -1756,7 +1756,7 @@ OB_ATTN_INSTANCES(128, false)
                                                                const int32_t *, int, int, int, float, float, int,  \
                                                                TileOrder, Band);                                   \
     OB_WINDOW_DKV(D, Band, dkv_np(D, 0), dkv_sr(D, 0))                                                              \
-    OB_WINDOW_DKV(D, Sinks, 2, dkv_sr(D, 1))                                                                        \
+    OB_WINDOW_DKV(D, Sinks, 2, SINK_SR)                                                                        \
     template __global__ void attn_sink_sum_kernel<D>(const float *, __bf16 *, __bf16 *, int, const int32_t *, int, Sinks, float);
 #define OB_WINDOW_DKV(D, W, NP, SR)                                                                               \
     template __global__ void attn_bwd_dkv_kernel<D, true, NP, SR, false, W>(const __bf16 *, const __bf16 *, const __bf16 *, \
@@ -1897,10 +1897,10 @@ void launch_attn_window_bwd(const void *d_o, const void *q, const void *k, const
     const dim3 grid_s((unsigned)chunks * nkv), grid_r(split, nkv, (2 * sinks * d + 255) / 256);
     ord.n = 0;
     if (d == 64) {
-        hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, 2, dkv_sr(64, 1), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
+        hipLaunchKernelGGL((attn_bwd_dkv_kernel<64, true, 2, SINK_SR, false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
         hipLaunchKernelGGL((attn_sink_sum_kernel<64>), grid_r, dim3(256), 0, s, part, (__bf16 *)dk, (__bf16 *)dv, ldkv, seg->cu_dev, seg->n_seg, first, scale);
     } else {
-        hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, 2, dkv_sr(128, 1), false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
+        hipLaunchKernelGGL((attn_bwd_dkv_kernel<128, true, 2, SINK_SR, false, Sinks>), grid_s, dim3(256), 0, s, OB_ARGS(first));
         hipLaunchKernelGGL((attn_sink_sum_kernel<128>), grid_r, dim3(256), 0, s, part, (__bf16 *)dk, (__bf16 *)dv, ldkv, seg->cu_dev, seg->n_seg, first, scale);
     }
 #undef OB_ARGS
