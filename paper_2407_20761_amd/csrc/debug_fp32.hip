@@ -202,20 +202,12 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(int swiglu, const float *_
 }
 
 // ---- attention: one wavefront per (row, head); lanes split the head dimension ------------------
-// A row sees keys [lo, hi) of its segment, with a window its last `window` and the segment's first `sinks` (NO_WINDOW: all).
-constexpr int NO_WINDOW = 1 << 30;
-// the key after j that row t sees, from the segment's start lo on
-__device__ __forceinline__ int next_key(int j, int t, int lo, int window, int sinks) {
-    ++j;
-    return t - j >= window && j - lo >= sinks ? t - window + 1 : j;
-}
-__device__ __forceinline__ int first_key(int t, int lo, int window, int sinks) { return next_key(lo - 1, t, lo, window, sinks); }
 // forward: online softmax over the allowed keys of the row's segment
 __global__ __launch_bounds__(256) void attn_fwd_kernel(const float *__restrict__ q, const float *__restrict__ k,
                                                        const float *__restrict__ v, float *__restrict__ o,
                                                        float *__restrict__ lse, int ldq, int ldkv, int ldo,
                                                        const int32_t *__restrict__ cu, int n_seg, int T, int nq,
-                                                       int group, int d, float scale, int causal, int window, int sinks) {
+                                                       int group, int d, float scale, int causal) {
     const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 6;
     const int lane = threadIdx.x & 63;
     if (w >= (long)T * nq) return;
@@ -226,7 +218,7 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(const float *__restrict__
     float qv[2] = {0.f, 0.f}, ov[2] = {0.f, 0.f};
     for (int e = 0; e < per; ++e) qv[e] = q[(size_t)t * ldq + head * d + lane + 64 * e];
     float m = -INFINITY, l = 0.f;
-    for (int j = first_key(t, lo, window, sinks); j < hi; j = next_key(j, t, lo, window, sinks)) {
+    for (int j = lo; j < hi; ++j) {
         float part = 0.f;
         for (int e = 0; e < per; ++e) part += qv[e] * k[(size_t)j * ldkv + kvh * d + lane + 64 * e];
         const float s = wave_sum(part) * scale;
@@ -262,7 +254,7 @@ __global__ __launch_bounds__(256) void attn_bwd_dq_kernel(const float *__restric
                                                           const float *__restrict__ lse, const float *__restrict__ delta,
                                                           float *__restrict__ dq, int ldq, int ldkv, int ldo,
                                                           const int32_t *__restrict__ cu, int n_seg, int T, int nq,
-                                                          int group, int d, float scale, int causal, int window, int sinks) {
+                                                          int group, int d, float scale, int causal) {
     const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 6;
     const int lane = threadIdx.x & 63;
     if (w >= (long)T * nq) return;
@@ -276,7 +268,7 @@ __global__ __launch_bounds__(256) void attn_bwd_dq_kernel(const float *__restric
         dov[e] = d_o[(size_t)t * ldo + head * d + lane + 64 * e];
     }
     const float ls = lse[(size_t)head * T + t], dl = delta[(size_t)head * T + t];
-    for (int j = first_key(t, lo, window, sinks); j < hi; j = next_key(j, t, lo, window, sinks)) {
+    for (int j = lo; j < hi; ++j) {
         float ps = 0.f, pd = 0.f;
         for (int e = 0; e < per; ++e) {
             const size_t off = (size_t)j * ldkv + kvh * d + lane + 64 * e;
@@ -291,23 +283,18 @@ __global__ __launch_bounds__(256) void attn_bwd_dq_kernel(const float *__restric
 }
 
 // dk[j, kvh] = scale sum_{heads of the group} sum_t dS_tj q_t;  dv[j, kvh] = sum sum P_tj dO_t
-// SHARED waves to a key row, each every SHARED-th of its queries (with sinks, a key that all of a long segment sees would keep the launch waiting)
-template <int SHARED>
 __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(const float *__restrict__ d_o, const float *__restrict__ q,
                                                            const float *__restrict__ k, const float *__restrict__ v,
                                                            const float *__restrict__ lse, const float *__restrict__ delta,
                                                            float *__restrict__ dk, float *__restrict__ dv, int ldq,
                                                            int ldkv, int ldo, const int32_t *__restrict__ cu, int n_seg,
-                                                           int T, int nkv, int group, int d, float scale, int causal,
-                                                           int window, int sinks) {
-    static_assert(SHARED == 1 || SHARED == 4, "a workgroup's four waves");
-    __shared__ float sums[SHARED == 4 ? 4 : 1][4][64];
-    const long w = SHARED == 4 ? (long)blockIdx.x : ((long)blockIdx.x * 256 + threadIdx.x) >> 6;
-    const int lane = threadIdx.x & 63, mine = SHARED == 4 ? threadIdx.x >> 6 : 0;
+                                                           int T, int nkv, int group, int d, float scale, int causal) {
+    const long w = ((long)blockIdx.x * 256 + threadIdx.x) >> 6;
+    const int lane = threadIdx.x & 63;
     if (w >= (long)T * nkv) return;
     const int j = (int)(w / nkv), kvh = (int)(w % nkv);
     const int sj = segment_of(cu, n_seg, j);
-    const int lo = causal ? j : cu[sj], hi = j - cu[sj] < sinks ? cu[sj + 1] : min(cu[sj + 1], j + window);
+    const int lo = causal ? j : cu[sj], hi = cu[sj + 1];
     const int per = d / 64;
     float kv_[2] = {0.f, 0.f}, vv[2] = {0.f, 0.f}, ak[2] = {0.f, 0.f}, av[2] = {0.f, 0.f};
     for (int e = 0; e < per; ++e) {
@@ -315,7 +302,7 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(const float *__restri
         vv[e] = v[(size_t)j * ldkv + kvh * d + lane + 64 * e];
     }
     for (int head = kvh * group; head < (kvh + 1) * group; ++head)
-        for (int t = lo + mine; t < hi; t += SHARED) {
+        for (int t = lo; t < hi; ++t) {
             float ps = 0.f, pd = 0.f, qe[2] = {0.f, 0.f}, de[2] = {0.f, 0.f};
             for (int e = 0; e < per; ++e) {
                 qe[e] = q[(size_t)t * ldq + head * d + lane + 64 * e];
@@ -327,13 +314,6 @@ __global__ __launch_bounds__(256) void attn_bwd_dkv_kernel(const float *__restri
             const float ds = p * (wave_sum(pd) - delta[(size_t)head * T + t]);
             for (int e = 0; e < per; ++e) { av[e] += p * de[e]; ak[e] += ds * qe[e]; }
         }
-    if (SHARED == 4) {
-        for (int e = 0; e < 2; ++e) { sums[mine][e][lane] = ak[e]; sums[mine][2 + e][lane] = av[e]; }
-        __syncthreads();
-        if (mine != 0) return;
-        for (int m = 1; m < 4; ++m)
-            for (int e = 0; e < 2; ++e) { ak[e] += sums[m][e][lane]; av[e] += sums[m][2 + e][lane]; }
-    }
     for (int e = 0; e < per; ++e) {
         dk[(size_t)j * ldkv + kvh * d + lane + 64 * e] = ak[e] * scale;
         dv[(size_t)j * ldkv + kvh * d + lane + 64 * e] = av[e];
@@ -395,48 +375,26 @@ void gemm(int layout, int M, int N, int K, const float *A, const float *B, float
 
 }  // namespace
 
-static void run_attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
-                         const ob_segments *seg, int nq, int nkv, int d, float scale, int causal, int window, int sinks, hipStream_t s) {
+void attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
+              const ob_segments *seg, int nq, int nkv, int d, float scale, int mask, hipStream_t s) {
     const int T = seg->total_tokens;
     hipLaunchKernelGGL(attn_fwd_kernel, dim3(blocks_for((long)T * nq * 64)), dim3(256), 0, s, (const float *)q,
                        (const float *)k, (const float *)v, (float *)o, lse, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T,
-                       nq, nq / nkv, d, scale, causal, window, sinks);
+                       nq, nq / nkv, d, scale, mask == OB_MASK_SEG_CAUSAL ? 1 : 0);
 }
 
-static void run_attn_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
-                         void *dq, void *dk, void *dv, float *delta, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
-                         int nkv, int d, float scale, int causal, int window, int sinks, hipStream_t s) {
-    const int T = seg->total_tokens;
+void attn_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
+              void *dq, void *dk, void *dv, float *delta, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
+              int nkv, int d, float scale, int mask, hipStream_t s) {
+    const int T = seg->total_tokens, causal = mask == OB_MASK_SEG_CAUSAL ? 1 : 0;
     hipLaunchKernelGGL(attn_delta_kernel, dim3(blocks_for((long)T * nq * 64)), dim3(256), 0, s, (const float *)d_o,
                        (const float *)o, ldo, delta, T, nq, d);
     hipLaunchKernelGGL(attn_bwd_dq_kernel, dim3(blocks_for((long)T * nq * 64)), dim3(256), 0, s, (const float *)d_o,
                        (const float *)q, (const float *)k, (const float *)v, lse, delta, (float *)dq, ldq, ldkv, ldo,
-                       seg->cu_dev, seg->n_seg, T, nq, nq / nkv, d, scale, causal, window, sinks);
-#define OB_ARGS (const float *)d_o, (const float *)q, (const float *)k, (const float *)v, lse, delta, (float *)dk, (float *)dv, ldq, ldkv, ldo, \
-                seg->cu_dev, seg->n_seg, T, nkv, nq / nkv, d, scale, causal, window, sinks
-    if (window < NO_WINDOW) hipLaunchKernelGGL((attn_bwd_dkv_kernel<4>), dim3((unsigned)((long)T * nkv)), dim3(256), 0, s, OB_ARGS);
-    else hipLaunchKernelGGL((attn_bwd_dkv_kernel<1>), dim3(blocks_for((long)T * nkv * 64)), dim3(256), 0, s, OB_ARGS);
-#undef OB_ARGS
-}
-
-void attn_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
-              const ob_segments *seg, int nq, int nkv, int d, float scale, int mask, hipStream_t s) {
-    run_attn_fwd(q, k, v, o, lse, ldq, ldkv, ldo, seg, nq, nkv, d, scale, mask == OB_MASK_SEG_CAUSAL ? 1 : 0, NO_WINDOW, 0, s);
-}
-void attn_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
-              void *dq, void *dk, void *dv, float *delta, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
-              int nkv, int d, float scale, int mask, hipStream_t s) {
-    run_attn_bwd(d_o, q, k, v, o, lse, dq, dk, dv, delta, ldq, ldkv, ldo, seg, nq, nkv, d, scale, mask == OB_MASK_SEG_CAUSAL ? 1 : 0,
-                 NO_WINDOW, 0, s);
-}
-void attn_window_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
-                     const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s) {
-    run_attn_fwd(q, k, v, o, lse, ldq, ldkv, ldo, seg, nq, nkv, d, scale, 1, window, sinks, s);
-}
-void attn_window_bwd(const void *d_o, const void *q, const void *k, const void *v, const void *o, const float *lse,
-                     void *dq, void *dk, void *dv, float *delta, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
-                     int nkv, int d, float scale, int window, int sinks, hipStream_t s) {
-    run_attn_bwd(d_o, q, k, v, o, lse, dq, dk, dv, delta, ldq, ldkv, ldo, seg, nq, nkv, d, scale, 1, window, sinks, s);
+                       seg->cu_dev, seg->n_seg, T, nq, nq / nkv, d, scale, causal);
+    hipLaunchKernelGGL(attn_bwd_dkv_kernel, dim3(blocks_for((long)T * nkv * 64)), dim3(256), 0, s, (const float *)d_o,
+                       (const float *)q, (const float *)k, (const float *)v, lse, delta, (float *)dk, (float *)dv, ldq,
+                       ldkv, ldo, seg->cu_dev, seg->n_seg, T, nkv, nq / nkv, d, scale, causal);
 }
 
 // Buffers of the fp32 block: the same members as the bf16 path, four bytes per element.

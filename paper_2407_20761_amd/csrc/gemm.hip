@@ -532,7 +532,8 @@ struct KLoop {
 // The last two are those of the cross entropy over a vocabulary, whose logits z = x W^T ("NT") are not stored:
 //   EPI_LOSS_STATS  per row of z and column half of a tile its maximum and the sum of exp(z - maximum): float2 [2 tiles_n][M] in place of C; the logit of
 //                   the row's label (in place of R) to float [M] in place of the bias, by the lane that holds it
-//   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) weight, zeros in the columns N .. ldc; LossRow [M] in place of R, ldr the label of column 0
+//   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) dnll, zeros in the columns N .. ldc; labels in place of R, dnll of the bias, lse of the slice
+//                   sums, ldr the label of column 0, n_tail of the slices the number of labels (the launch has whole tiles only)
 enum { EPI_PLAIN = 0, EPI_ROWS, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD, EPI_LOSS_STATS, EPI_LOSS_GRAD };
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -685,30 +686,35 @@ __device__ __forceinline__ void gemm_tile(
                 *(f32x4 OB_LDS *)(slab + (16 * h + lx) * RSTR + (j * 16 + lq * 4) * 4) = acc[2 * ii + h][j];
     };
     if constexpr (EPI == EPI_LOSS_GRAD) {
+        const int32_t *labels = (const int32_t *)side;
+        const float *lse = ts.part, *dnll = (const float *)bias;
         put(0);
 #pragma unroll
         for (int ii = 0; ii < TA / 2; ++ii) {
             constexpr int NR = 32 / RPI;
             f32x4 lo[NR], hi[NR];
-            LossRow of[NR];
+            float lse2[NR], weight[NR];
+            int label[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
-                const int row = r * RPI + lane / LPR, m = m0 + wm * (BM / WM) + ii * 32 + row;
+                const int row = r * RPI + lane / LPR, m = min(m0 + wm * (BM / WM) + ii * 32 + row, M - 1);
                 lo[r] = *(const f32x4 OB_LDS *)(slab + row * RSTR + (lane % LPR) * 32);
                 hi[r] = *(const f32x4 OB_LDS *)(slab + row * RSTR + (lane % LPR) * 32 + 16);
-                of[r] = m < M ? ((const LossRow *)side)[m] : LossRow{0.f, 0.f, -1, 0};
+                label[r] = labels[m];
+                lse2[r] = lse[m] * LOG2E;
+                weight[r] = label[r] >= 0 && label[r] < ts.n_tail ? dnll[m] : 0.f;
             }
             if (ii + 1 < TA / 2) put(ii + 1);
 #pragma unroll
             for (int r = 0; r < NR; ++r) {
-                const int m = m0 + wm * (BM / WM) + ii * 32 + r * RPI + lane / LPR, rel = of[r].label - ldr - n_out;
+                const int m = m0 + wm * (BM / WM) + ii * 32 + r * RPI + lane / LPR, rel = label[r] - ldr - n_out;
                 bf16x8 g;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float z = e < 4 ? lo[r][e & 3] : hi[r][e & 3];
                     // (a row without a label has weight 0: its logits may be anything)
-                    const float p = __builtin_amdgcn_exp2f(z * LOG2E - of[r].lse2) - (e == rel ? 1.f : 0.f);
-                    g[e] = (__bf16)(of[r].weight == 0.f || n_out + e >= N ? 0.f : p * of[r].weight);
+                    const float p = __builtin_amdgcn_exp2f(z * LOG2E - lse2[r]) - (e == rel ? 1.f : 0.f);
+                    g[e] = (__bf16)(weight[r] == 0.f || n_out + e >= N ? 0.f : p * weight[r]);
                 }
                 if (m < M && n_out < ldc) *(bf16x8 *)(Cm + (size_t)m * ldc + n_out) = g;
             }
@@ -1163,9 +1169,8 @@ int gemm_any(int layout, int M, int N, int K, const void *A, const void *B, void
 // z = A B^T, [M, N] over K, in whole tiles of p (loss_plan), in pieces of the columns where the caller cuts B
 template <int EPI>
 static void launch_loss(const Plan &p, int M, int N, int K, const void *A, const void *B, void *C, int ldc, const void *bias, const void *side,
-                        int ldr, hipStream_t s) {
+                        int ldr, const TailSplit &ts, hipStream_t s) {
     ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
-    const TailSplit ts{nullptr, 0, 0, 1, 0};
     const int tm = (M + tile_rows(p.kind) - 1) / tile_rows(p.kind), tn = (N + tile_cols(p.kind) - 1) / tile_cols(p.kind);
 #define OB_ARGS dim3(tm * tn), dim3(256), 0, s, M, N, K, (const __bf16 *)A, K, (const __bf16 *)B, K, (__bf16 *)C, ldc, (const __bf16 *)bias,  \
                 (const __bf16 *)side, ldr, tm, tn, ts
@@ -1176,11 +1181,11 @@ static void launch_loss(const Plan &p, int M, int N, int K, const void *A, const
 }
 void launch_loss_stats(const Plan &p, int n, int V, int H, const void *x, const void *w, const int32_t *labels, void *stats, float *target,
                        hipStream_t s) {
-    launch_loss<EPI_LOSS_STATS>(p, n, V, H, x, w, stats, 0, target, labels, 0, s);
+    launch_loss<EPI_LOSS_STATS>(p, n, V, H, x, w, stats, 0, target, labels, 0, TailSplit{nullptr, 0, 0, 1, 0}, s);
 }
-void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, const void *w, const LossRow *rows, int first, void *g, int ldg,
-                      hipStream_t s) {
-    launch_loss<EPI_LOSS_GRAD>(p, n, cols, H, x, w, g, ldg, nullptr, rows, first, s);
+void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, const void *w, const int32_t *labels, int V, const float *lse,
+                      const float *dnll, int first, void *g, int ldg, hipStream_t s) {
+    launch_loss<EPI_LOSS_GRAD>(p, n, cols, H, x, w, g, ldg, dnll, labels, first, TailSplit{(float *)lse /* read only */, p.n_full, V, 1, 0}, s);
 }
 
 // "NN" and "TN" with operands whose rows are longer than the product's; ws: as for gemm_any()

@@ -61,14 +61,6 @@ __global__ __launch_bounds__(256) void loss_combine_kernel(const float2 *__restr
     nll[row] = label >= 0 && label < V ? l - target[row] : 0.f;
 }
 
-__global__ __launch_bounds__(256) void loss_rows_kernel(const float *__restrict__ lse, const float *__restrict__ dnll,
-                                                        const int32_t *__restrict__ labels, int n, int V, LossRow *__restrict__ rows) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const int label = labels[i];
-    rows[i] = LossRow{lse[i] * LOG2E, label >= 0 && label < V ? dnll[i] : 0.f, label, 0};
-}
-
 // one wave to a row of `big`: its place in the list by bisection
 __global__ __launch_bounds__(256) void rows_spread_kernel(const __bf16 *__restrict__ small, __bf16 *__restrict__ big,
                                                           const int32_t *__restrict__ rows, int n_rows, int T, int H) {
@@ -97,10 +89,6 @@ void launch_loss_combine(const void *stats, const float *target, const int32_t *
         hipLaunchKernelGGL((loss_combine_kernel<4>), dim3((n + 3) / 4), dim3(256), 0, s, (const float2 *)stats, target, labels, n, V, slots, nll, lse);
     else
         hipLaunchKernelGGL((loss_combine_kernel<16>), dim3((n + 15) / 16), dim3(256), 0, s, (const float2 *)stats, target, labels, n, V, slots, nll, lse);
-}
-void launch_loss_rows(const float *lse, const float *dnll, const int32_t *labels, int n, int V, LossRow *rows, hipStream_t s) {
-    ProfScope prof(K_ROWS, s, 28.0 * n);
-    hipLaunchKernelGGL(loss_rows_kernel, dim3((n + 255) / 256), dim3(256), 0, s, lse, dnll, labels, n, V, rows);
 }
 void launch_rows_spread(const void *small, void *big, const int32_t *rows_dev, int n_rows, int T, int H, hipStream_t s) {
     ProfScope prof(K_ROWS, s, 2.0 * H * ((double)T + n_rows));

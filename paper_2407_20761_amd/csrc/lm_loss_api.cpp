@@ -31,7 +31,7 @@ struct Pieces {
 
 int slots_of(const Plan &p, int V) { return 2 * ((V + tile_cols(p.kind) - 1) / tile_cols(p.kind)); }
 
-struct Work { size_t xs, stats, target, rows, g, dxs, sums, sums_bytes, total; };
+struct Work { size_t xs, stats, target, g, dxs, sums, sums_bytes, total; };
 Work work_layout(int n, int V, int H) {
     const Plan logits = whole_plan(0, n, V, H);
     const Pieces pc(n, V);
@@ -41,7 +41,6 @@ Work work_layout(int n, int V, int H) {
     Bump bwd = fwd;
     w.stats = fwd.take((size_t)slots_of(logits, V) * n * 8);
     w.target = fwd.take((size_t)n * 4);
-    w.rows = bwd.take((size_t)n * sizeof(LossRow));
     w.dxs = bwd.take((size_t)n * H * 2);
     w.g = bwd.take((size_t)n * pc.ld * 2);
     if (pc.count > 1) {
@@ -144,8 +143,6 @@ extern "C" int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void
         xs = at + wk.xs;
         dxs = at + wk.dxs;
     }
-    LossRow *rows = (LossRow *)(at + wk.rows);
-    launch_loss_rows(lse, dnll, labels, n, V, rows, s);
     // Per piece of the vocabulary: G = (softmax - one-hot) weight, its logits computed again; dW rows of the piece = G^T x, whole; dx += G W
     const Plan p_dx = whole_plan(1, n, H, pc.cols);
     float *sums = (float *)(at + wk.sums);
@@ -154,7 +151,7 @@ extern "C" int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void
         const int v0 = i * pc.cols, cols = V - v0 < pc.cols ? V - v0 : pc.cols, ld = (cols + 63) / 64 * 64;
         const unsigned char *wp = (const unsigned char *)w + (size_t)v0 * H * 2;
         unsigned char *dwp = (unsigned char *)dw + (size_t)v0 * H * 2;
-        launch_loss_grad(whole_plan(0, n, cols, H), n, cols, H, xs, wp, rows, v0, g, ld, s);
+        launch_loss_grad(whole_plan(0, n, cols, H), n, cols, H, xs, wp, labels, V, lse, dnll, v0, g, ld, s);
         launch_gemm_tn(cols, H, n, g, ld, xs, dwp, acc ? dwp : nullptr, s);
         if (pc.count > 1) launch_gemm_nn_piece(p_dx, n, H, cols, g, ld, wp, sums, i, s);
         else launch_gemm_nn(n, H, cols, g, ld, wp, dxs, wk.sums_bytes ? sums : nullptr, wk.sums_bytes, s);

@@ -57,14 +57,13 @@ int gemm_tn_group(int count, const GemmTN *g, int K, void *ws, size_t ws_bytes, 
 
 // ---- cross entropy over a vocabulary (gemm.hip: the products; lm_loss.hip: the row kernels) --------
 struct Plan;
-// of a row: its log-sum-exp in base-2 units, the gradient of its loss (0: it has no label), its label
-struct __attribute__((aligned(16))) LossRow { float lse2, weight; int32_t label, unused; };
 // x [n, H], w [V, H]; stats: float2 [2 column tiles of p][n], target [n]: the labels' logits
 void launch_loss_stats(const Plan &p, int n, int V, int H, const void *x, const void *w, const int32_t *labels, void *stats, float *target,
                        hipStream_t s);
-// g [n, ldg]: the gradient of the logits of `cols` columns, `first` the first one's label, w its row of weights; ldg = cols up to a multiple of 64
-void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, const void *w, const LossRow *rows, int first, void *g, int ldg,
-                      hipStream_t s);
+// g [n, ldg]: the gradient of the logits of `cols` of the V columns, `first` the first one's label, w its row of weights; ldg = cols up to a
+// multiple of 64
+void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, const void *w, const int32_t *labels, int V, const float *lse,
+                      const float *dnll, int first, void *g, int ldg, hipStream_t s);
 // C [M, N] = A [M, K] (row stride lda, zeros from K to a multiple of 64) B [K, N]; C = A [K, M]^T B [K, N] (+ R)
 void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *B, void *C, void *ws, size_t ws_bytes, hipStream_t s);
 void launch_gemm_tn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *R, hipStream_t s);
@@ -74,7 +73,6 @@ void launch_gemm_nn_sum(const Plan &p, int M, int N, float *part, int pieces, vo
 // stats of `slots` parts of the vocabulary and the labels' logits -> lse, nll (0 for a row without a label)
 void launch_loss_combine(const void *stats, const float *target, const int32_t *labels, int n, int V, int slots, float *nll, float *lse,
                          hipStream_t s);
-void launch_loss_rows(const float *lse, const float *dnll, const int32_t *labels, int n, int V, LossRow *rows, hipStream_t s);
 // big [T, H]: row rows[i] (ascending) = small[i], the others zeros
 void launch_rows_spread(const void *small, void *big, const int32_t *rows_dev, int n_rows, int T, int H, hipStream_t s);
 
