@@ -366,6 +366,7 @@ __device__ __forceinline__ float start_of(uint32_t hidden, int c) {
 template <class WIN>
 struct BandTiles {
     static constexpr int skip = 0, n_head = 0, window = 0, sink_end = 0;
+    static constexpr bool few_sinks = false;
     __device__ __forceinline__ BandTiles(const TileInfo &, const WIN &, int) {}
     __device__ __forceinline__ int row(int j) const { return j * ST; }       // first key row of tile j, from the segment's start
     __device__ __forceinline__ bool wave_sees(int, int) const { return true; }      // some row of the wave, keys of the band in these
@@ -373,7 +374,7 @@ struct BandTiles {
 template <>
 struct BandTiles<Band> {
     int window, skip, n_head, sink_end, wave_from;
-    bool apart;          // the sinks have a tile of their own
+    bool apart, few_sinks;          // the sinks have a tile of their own, and lie in its first 32 rows
     __device__ __forceinline__ BandTiles(const TileInfo &ti, const Band &win, int wave) {
         window = win.window;
         sink_end = min(ti.seg_start + win.sinks, ti.seg_end);
@@ -382,6 +383,7 @@ struct BandTiles<Band> {
         const int first = max(0, len_front - window + 1) / ST;               // first tile of the band
         const int whole = max(0, last - window + 1 + ST - 1) / ST;           // first that lies in every row's window
         apart = first > 0 && win.sinks > 0;
+        few_sinks = apart && win.sinks <= 32;
         skip = apart ? first - 1 : first;
         n_head = min(whole, (last + ST) / ST) - skip;
     }
@@ -401,7 +403,8 @@ struct BandTiles<Band> {
 
 // BAND: a row sees its last `window` keys and those below sink_end.  As an unsigned number the distance from key to row is below the
 // window for just the keys of the band, those behind the row and past the segment's end left out: one comparison.
-template <int D, bool CAUSAL, bool MASK, bool BAND = false>
+// KB: 32-row blocks of the tile that are looked at.
+template <int D, bool CAUSAL, bool MASK, bool BAND = false, int KB = 2>
 __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict__ ks,
                                          const unsigned char OB_LDS *__restrict__ vs, const Tile<D> &tl,
                                          const bf16x8 (&qf)[D / 16], f32x16 (&acc_o)[D / 32], float &m_run,
@@ -410,11 +413,11 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
     constexpr int HB = 2;                 // K fragments (D-steps) per batch
     constexpr int R = D == 128 ? 3 : 2;   // batches in flight (ring depth)
     constexpr int PER = (D / 16) / HB;    // batches per 32-row tile
-    constexpr int NB = 2 * PER;
+    constexpr int NB = KB * PER;
     constexpr int DT = D / 32;
-    f32x16 acc_s[2];
+    f32x16 acc_s[KB];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < KB; ++mt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc_s[mt][r] = 0.f;
     bf16x8 fa[R][HB], fb[2][DT];
@@ -445,7 +448,7 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
     const int dist = q_row - kv0 - 4 * lh, below = min(sink_end - kv0 - 4 * lh, dist + 1);
     if (MASK) {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < KB; ++mt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int kv = kv0 + mt * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
@@ -457,7 +460,7 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
             }
     } else {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+        for (int mt = 0; mt < KB; ++mt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, acc_s[mt][r]);
     }
@@ -496,9 +499,9 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
     bf16x8 pb = probs(0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < ST / 16; ++u) {
+    for (int u = 0; u < 2 * KB; ++u) {
         bf16x8 pn = pb;
-        if (u + 1 < ST / 16) {
+        if (u + 1 < 2 * KB) {
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) fb[(u + 1) & 1][dt] = tl.frag_tr(vs, dt, u + 1);
             pn = probs(u + 1);
@@ -506,7 +509,7 @@ __device__ __forceinline__ void fwd_tile(const unsigned char OB_LDS *__restrict_
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
             acc_o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[u & 1][dt], pb, acc_o[dt], 0, 0, 0);
-        if (u + 1 < ST / 16) {
+        if (u + 1 < 2 * KB) {
             __builtin_amdgcn_sched_group_barrier(0x100, 2 * DT, 0);        // next step's V fragments
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) {
@@ -596,6 +599,15 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
     }
 #define OB_FWD_ANY(MASKED) OB_FWD_ITER(MASKED, (j & 1) ? ks1 : ks0, (j & 1) ? vs1 : vs0, (j & 1) ? ks0 : ks1, (j & 1) ? vs0 : vs1)
     if constexpr (WIN::BAND) {
+        if (bt.few_sinks) {      // half a tile will do for the sinks
+            __builtin_amdgcn_s_waitcnt(WAIT_VM0);
+            __syncthreads();
+            const long off = (long)(ti.seg_start + bt.row(1)) * ldkv * 2;
+            tl.issue(kbase + off, kv_bytes - off, ks1, wave);
+            tl.issue(vbase + off, kv_bytes - off, vs1, wave);
+            fwd_tile<D, CAUSAL, true, true, 1>(ks0, vs0, tl, qf, acc_o, m_run, l_run, ti.seg_start, ti.seg_end, q_row, sl2, bt.window, bt.sink_end);
+            j = 1;
+        }
         while (j < bt.n_head) OB_FWD_ANY(true)
         if ((j & 1) && j < n_main) OB_FWD_ANY(false)
     }
