@@ -276,8 +276,9 @@ __device__ __forceinline__ int head_of_slot(int hs, int heads) {
 // workgroup gives each segment's first tile number, and the thread whose range holds `tile`
 // publishes the answer -- one global-memory round trip instead of a serial walk over cu.
 struct TileInfo { int seg_start, seg_end, row0; };
-// LONGER: segments of at most `longer_than` rows have no tiles.
-template <bool LONGER = false>
+// OF: tiles of the segments, or, of those longer than `longer_than` alone, the chunks of the sinks' sums, or the whole segment as one tile.
+enum { TILES = 0, SINK_CHUNKS, SINK_SEGMENTS };
+template <int OF = TILES>
 __device__ __forceinline__ TileInfo find_tile(const int32_t *__restrict__ cu, int n_seg, int tile_rows,
                                               int *sh /* >= 8 ints */, int tile, int longer_than = 0) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -290,7 +291,8 @@ __device__ __forceinline__ TileInfo find_tile(const int32_t *__restrict__ cu, in
         if (scans && j < n_seg) {
             a = cu[j];
             b = cu[j + 1];
-            nt = !LONGER || b - a > longer_than ? (b - a + tile_rows - 1) / tile_rows : 0;
+            if (OF == SINK_CHUNKS) tile_rows = sink_chunk_rows(b - a);
+            nt = OF == TILES ? (b - a + tile_rows - 1) / tile_rows : b - a <= longer_than ? 0 : OF == SINK_SEGMENTS ? 1 : (b - a + tile_rows - 1) / tile_rows;
         }
         int incl = nt;  // inclusive scan inside the wave
 #pragma unroll
@@ -343,7 +345,7 @@ __device__ __forceinline__ TileInfo pick_tile(const TileOrder &ord, int rank, co
 // not a number, can reach it.
 struct Whole { static constexpr bool BAND = false, SINKS = false; };
 struct Band { static constexpr bool BAND = true, SINKS = false; int window, sinks, whole; };      // whole: see sink_whole_rows()
-struct Sinks { static constexpr bool BAND = false, SINKS = true; int whole, sinks, chunk; float *part; };
+struct Sinks { static constexpr bool BAND = false, SINKS = true; int whole, sinks; float *part; };
 
 // ------------------------------------------------------------------------------------------------
 // forward:  S^T = K Q^T,  online softmax per lane,  O^T += V^T P^T
@@ -1239,7 +1241,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 && SR == 32 ? 2 : D == 128 || NP
     TileInfo ti;
     int q_chunk = 0;          // (Sinks) first of the workgroup's query rows
     if constexpr (WIN::SINKS) {
-        ti = find_tile<true>(cu, n_seg, win.chunk, sh, rank, win.whole);
+        ti = find_tile<SINK_CHUNKS>(cu, n_seg, 0, sh, rank, win.whole);
         q_chunk = ti.row0;
         ti.row0 = ti.seg_start;
     } else {
@@ -1258,7 +1260,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 && SR == 32 ? 2 : D == 128 || NP
     constexpr bool HIDE = WIN::BAND || WIN::SINKS;
     const BandRows<WIN> rows(ti, win, KVT, dkv_whole(D), pair_kv_first, kv_row);
     int q_end = WIN::BAND ? rows.q_end : ti.seg_end;
-    if constexpr (WIN::SINKS) q_end = min(ti.seg_end, q_chunk + win.chunk);
+    if constexpr (WIN::SINKS) q_end = min(ti.seg_end, q_chunk + sink_chunk_rows(ti.seg_end - ti.seg_start));
     const int rows_end = HIDE ? q_end : T;
     const float sl2 = scale * LOG2E;
     constexpr int KT = D / 16, DT = D / 32;
@@ -1672,17 +1674,17 @@ __global__ __launch_bounds__(256) void attn_sink_sum_kernel(const float *__restr
     __shared__ int sh[8];
     __shared__ f32x4 quarter[4][64];
     const int kvh = blockIdx.y, nkv = gridDim.y;
-    const TileInfo ti = find_tile<true>(cu, n_seg, MAX_TOKENS, sh, blockIdx.x, win.whole);
+    const TileInfo ti = find_tile<SINK_SEGMENTS>(cu, n_seg, 0, sh, blockIdx.x, win.whole);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = (blockIdx.z * 64 + lane) * 4;
     // chunks of the segments in front of it
     int slot0 = 0;
     for (int j = lane; j < n_seg && cu[j] < ti.seg_start; j += 64) {
         const int n = cu[j + 1] - cu[j];
-        slot0 += n > win.whole ? (n + win.chunk - 1) / win.chunk : 0;
+        slot0 += n > win.whole ? sink_chunks_of(n) : 0;
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) slot0 += __shfl_xor(slot0, o);
-    const int len = ti.seg_end - ti.seg_start, chunks = (len + win.chunk - 1) / win.chunk;
+    const int len = ti.seg_end - ti.seg_start, chunks = sink_chunks_of(len);
     const int role = e / (win.sinks * D), r = e - role * win.sinks * D;
     const bool live = role < 2 && r / D < len;
     const size_t slot = (size_t)nkv * 2 * win.sinks * D;
@@ -1905,7 +1907,7 @@ void launch_attn_window_bwd(const void *d_o, const void *q, const void *k, const
     int split;
     const int chunks = sink_chunks(seg, whole, sinks, &split);
     if (!chunks) return;
-    const Sinks first{whole, sinks, SINK_CHUNK, part};
+    const Sinks first{whole, sinks, part};
     const dim3 grid_s((unsigned)chunks * nkv), grid_r(split, nkv, (2 * sinks * d + 255) / 256);
     ord.n = 0;
     if (d == 64) {

@@ -61,7 +61,7 @@ int sink_chunks(const ob_segments *seg, int whole, int sinks, int *segments) {
     for (int j = 0; j < seg->n_seg && sinks; ++j) {
         const int len = seg->cu_host[j + 1] - seg->cu_host[j];
         if (len <= whole) continue;
-        n += (len + SINK_CHUNK - 1) / SINK_CHUNK;
+        n += sink_chunks_of(len);
         ++split;
     }
     if (segments) *segments = split;

@@ -55,8 +55,11 @@ int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal, in
 constexpr int MAX_SINKS = 64;      // they lie in a segment's first tile of keys
 // The sinks of a segment are seen by all of its rows.  Up to sink_whole_rows() the workgroup of its first keys walks them all: what that adds to its
 // walk, rows past the window times the heads of a group, is to cost less than the two launches of the other way (about 25 trips of 64 rows).
-// Beyond, chunks of SINK_CHUNK rows leave fp32 sums.  Both are the segment's own, so that it gives the same sums in every batch.
-constexpr int SINK_CHUNK = 256, SINK_SR = 32;      // (query rows of a streamed tile)
+// Beyond, chunks of its rows leave fp32 sums, of 128 rows while that is few chunks (one segment of 557, 32 / 8 heads of 128, window 128: dK / dV 54 -> 45 us
+// against 256; one of 65521, 64 sinks, window 512 420 -> 437).  All of this is the segment's own, so that it gives the same sums in every batch.
+constexpr int SINK_SR = 32;      // query rows of a streamed tile
+__host__ __device__ constexpr int sink_chunk_rows(int len) { return len <= 4096 ? 128 : 256; }
+__host__ __device__ constexpr int sink_chunks_of(int len) { return (len + sink_chunk_rows(len) - 1) / sink_chunk_rows(len); }
 constexpr int sink_whole_rows(int window, int group) { return window + 1600 / group; }
 // chunks of all the segments that have them, and how many segments that are
 int sink_chunks(const ob_segments *seg, int whole, int sinks, int *segments = nullptr);

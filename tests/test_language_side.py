@@ -268,7 +268,7 @@ def test_workspace_and_the_blocks_own_refusals():
     own = ob.ob_block_workspace_bytes(desc, 2000)
     assert ob.ob_block_attn_workspace_bytes(desc, plain, seg) == own
     need = ob.ob_block_attn_workspace_bytes(desc, windowed, seg)
-    assert need == own + 8 * 2 * 4 * 64 * 4              # eight chunks of 256 rows, one key/value head
+    assert need == own + 16 * 2 * 4 * 64 * 4             # sixteen chunks of 128 rows, one key/value head
     w, g, p = ob.ob_block_weights(*[0x1000] * 12), ob.ob_block_grads(*[0x1000] * 12), C.c_void_p(0x1000)
     call = lambda d, s, n, ws: ob.lib.ob_block_attn_bwd(d, C.byref(windowed.c), C.byref(w), C.byref(g), 0, p, p, p, p, 1 << 40, s, ws, n, None)
     assert call(C.byref(desc), C.byref(seg.c), need - 1, p) == ob.OB_EWORKSPACE

@@ -96,6 +96,7 @@ CASES = [
     ([1], 1, 1, 64, 1, 0), ([1], 8, 1, 128, 5, 64), ([5], 2, 1, 64, 2, 64), ([2], 2, 1, 128, 1, 1),
     # several chunks of a segment's queries, tiles of the band without a mask, an odd and an even number of masked ones in front
     ([1100], 2, 1, 64, 200, 3), ([1100], 2, 1, 128, 200, 3), ([1500, 257], 4, 1, 64, 513, 16), ([1500, 257], 4, 1, 128, 512, 16),
+    ([4200, 150], 1, 1, 64, 70, 9), ([4200, 300], 1, 1, 128, 130, 64),
     ([900], 6, 1, 64, 90, 40), ([900], 6, 1, 128, 447, 64), ([2101], 1, 1, 128, 700, 8), ([2101], 1, 1, 64, 1030, 0),
 ]
 
@@ -270,7 +271,8 @@ def test_workspace_bytes():
     rows = 2 * up(1000 * 2 * 4)
     assert size(seg(1000), 2, 1, 64, 1000, 4) == rows                      # no segment is longer than the window
     assert size(seg(1000), 2, 1, 64, 100, 0) == rows                       # no sinks
-    assert size(seg(1000), 2, 1, 64, 100, 4) == rows + up(4 * 2 * 4 * 64 * 4)      # four chunks of 256 queries
+    assert size(seg(1000), 2, 1, 64, 100, 4) == rows + up(8 * 2 * 4 * 64 * 4)      # eight chunks of 128 queries
+    assert size(seg(5000), 2, 1, 64, 100, 4) == 2 * up(5000 * 2 * 4) + up(20 * 2 * 4 * 64 * 4)      # twenty of 256
     assert size(seg(1000), 2, 1, 64, 100, 4, ob.OB_FP32) == up(1000 * 2 * 4)
     assert size(seg(1000), 2, 1, 64, 0, 4) == 0 and size(seg(1000), 2, 1, 96, 5, 4) == 0
 
@@ -288,11 +290,11 @@ def _plan(lens, *a):
 
 # every kernel of dK / dV has cases in test_forward_and_backward: (its case) -> key rows, query rows, threads, chunks of the sinks
 REACHED = [
-    (([1100], 2, 1, 64, 200, 3), (64, 64, 256, 5)), (([1500, 257], 4, 1, 64, 513, 16), (64, 64, 256, 6)),
-    (([1100], 2, 1, 128, 200, 3), (64, 64, 512, 5)), (([2101], 1, 1, 128, 700, 8), (64, 64, 512, 0)),
-    (([900], 6, 1, 128, 447, 64), (64, 64, 512, 4)),
+    (([1100], 2, 1, 64, 200, 3), (64, 64, 256, 9)), (([1500, 257], 4, 1, 64, 513, 16), (64, 64, 256, 12)),
+    (([1100], 2, 1, 128, 200, 3), (64, 64, 512, 9)), (([2101], 1, 1, 128, 700, 8), (64, 64, 512, 0)),
+    (([900], 6, 1, 128, 447, 64), (64, 64, 512, 8)),
     # a full chip
-    (([2000] * 4, 16, 8, 64, 600, 4), (64, 32, 256, 32)), (([2000] * 4, 16, 8, 128, 600, 4), (128, 64, 512, 32)),
+    (([2000] * 4, 16, 8, 64, 600, 4), (64, 32, 256, 64)), (([2000] * 4, 16, 8, 128, 600, 4), (128, 64, 512, 64)),
     (([1100] * 4, 16, 8, 128, 600, 4), (64, 64, 512, 0)),
 ]
 
