@@ -135,7 +135,7 @@ int ob_varlen_attn_bwd_static(const void *d_o, const void *q, const void *k, con
 /* ---- varlen attention with a sliding window and sinks ------------------------------------------
  * As above, causal, with allowed(i, j) <=> same segment, j <= i, and (i - j < window or j is one of the segment's first
  * `sinks` tokens).  window >= 1 (a row sees itself: none is empty; a window as long as the segments is plain causal
- * attention), 0 <= sinks <= 64, scale > 0; row strides up to 2^24 elements, tensors and workspace aligned to 16 bytes.  Key
+ * attention), 0 <= sinks <= 64, 1e-20 <= scale <= 1e6; row strides up to 2^24 elements, tensors and workspace aligned to 16 bytes.  Key
  * tiles that no row of a workgroup sees are not computed, so a call costs tokens * window, not tokens^2.  Nothing of another segment is
  * read on a segment's behalf; inside a segment an infinity or NaN in a row of k, v or d_o may also reach rows near it that do not see it.
  * The backward's workspace (ob_varlen_attn_window_bwd_workspace_bytes for the same arguments; 0 if they are refused) holds the
@@ -274,10 +274,11 @@ int ob_connector_bwd(const ob_connector_desc *desc, const ob_connector_weights *
  * nll_r = lse_r - z_r,label, and for the gradients dnll_r of the losses
  *   G_rv = (exp(z_rv - lse_r) - [v = label_r]) dnll_r,   dx_r = sum_v G_rv W_v,   dW_v = sum_r G_rv x_r
  * The logits are never stored: the forward reduces each tile of them where it is computed, the backward computes them again
- * a piece of the vocabulary at a time (at most 1 GiB of G in bf16; fp32 sums of dx over the pieces, added in order).  No
+ * a piece of the vocabulary at a time (at most 1 GiB of G in bf16; dx is summed over the pieces in fp32, in order).  No
  * atomics: results are bitwise reproducible.
  * x [total_tokens, hidden], w [vocab, hidden].  rows (int32, n_rows entries, host and device copies): the supervised rows,
- * ascending, checked on the host; both NULL: every row (n_rows = total_tokens).  Visual tokens and prompts have no label, so a
+ * ascending, checked on the host; both NULL: every row (n_rows = total_tokens).  n_rows = 0 is a batch without a supervised
+ * row: nothing is read but the sizes, dx and (without OB_BWD_ACCUMULATE) dw are zeros.  Visual tokens and prompts have no label, so a
  * packed batch has far fewer rows here than tokens.  labels, nll, lse, dnll: device memory, n_rows entries.  A row whose label is
  * outside [0, vocab) is ignored: nll 0, no gradient whatever its dnll (x of a listed row has to be finite).
  * ob_lm_loss_bwd, given lse of the forward, writes every row of dx (rows not listed: zeros) and dw (flags: OB_BWD_ACCUMULATE

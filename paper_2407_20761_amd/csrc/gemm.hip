@@ -534,7 +534,8 @@ struct KLoop {
 //                   the row's label (in place of R) to float [M] in place of the bias, by the lane that holds it
 //   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) dnll, zeros in the columns N .. ldc; labels in place of R, dnll of the bias, lse of the slice
 //                   sums, ldr the label of column 0, n_tail of the slices the number of labels (the launch has whole tiles only)
-enum { EPI_PLAIN = 0, EPI_ROWS, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD, EPI_LOSS_STATS, EPI_LOSS_GRAD };
+// EPI_ADD_SUMS: a launch of slices adds its sums to those that are there ("NN": dx over the pieces of the vocabulary).
+enum { EPI_PLAIN = 0, EPI_ROWS, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD, EPI_LOSS_STATS, EPI_LOSS_GRAD, EPI_ADD_SUMS };
 constexpr float LOG2E = 1.4426950408889634f;
 
 // EPI_LOSS_STATS, straight from the accumulators: a lane holds, of rows 16 i + lane % 16, columns 16 j + 4 (lane / 16) .. + 3 of the wave's part, so a
@@ -760,7 +761,7 @@ __device__ __forceinline__ void gemm_tile(
             if (ii + 1 < TA / 2) put(ii + 1);
             const int m_first = m0 + wm * (BM / WM) + ii * 32 + lane / LPR;
             bf16x8 r8[NR], g8[NR];
-            if (EPI >= EPI_GELU_BWD) {
+            if constexpr (EPI == EPI_GELU_BWD || EPI == EPI_SWIGLU_BWD) {
 #pragma unroll
                 for (int r = 0; r < NR; ++r)
                     if (!CHECK || (m_first + r * RPI < M && n_out < N)) {
@@ -774,6 +775,10 @@ __device__ __forceinline__ void gemm_tile(
                 const int m = m_first + r * RPI;
                 if (MODE == 2) {
                     float *dst = ts.part + ((size_t)(kz * ts.n_tail + tail_tile) * BM + (m - m0)) * BN + (n_out - n0);
+                    if constexpr (EPI == EPI_ADD_SUMS) {
+                        lo[r] += *(const f32x4 *)dst;
+                        hi[r] += *(const f32x4 *)(dst + 4);
+                    }
                     *(f32x4 *)dst = lo[r];
                     *(f32x4 *)(dst + 4) = hi[r];
                 } else if (!CHECK || (m < M && n_out < N)) {
@@ -820,7 +825,8 @@ __device__ __forceinline__ void gemm_tile(
     };
     using std::integral_constant;
     const bool inside = m0 + BM <= M && n0 + BN <= N;
-    if constexpr (EPI >= EPI_LOSS_STATS) return;      // (above)
+    if constexpr (EPI == EPI_ADD_SUMS) out(integral_constant<int, 2>{}, integral_constant<bool, false>{});
+    else if constexpr (EPI >= EPI_LOSS_STATS) return;      // (above)
     else if constexpr (EPI >= EPI_GELU) {
         if (inside) out(integral_constant<int, 0>{}, integral_constant<bool, false>{});
         else out(integral_constant<int, 0>{}, integral_constant<bool, true>{});
@@ -941,6 +947,9 @@ OB_GEMM_INSTANCE(64, 64, false, false, 8, EPI_LOSS_STATS)
 OB_GEMM_INSTANCE(256, 256, false, false, 4, EPI_LOSS_GRAD)
 OB_GEMM_INSTANCE(128, 128, false, false, 4, EPI_LOSS_GRAD)
 OB_GEMM_INSTANCE(64, 64, false, false, 8, EPI_LOSS_GRAD)
+OB_GEMM_INSTANCE(256, 256, false, true, 4, EPI_ADD_SUMS)
+OB_GEMM_INSTANCE(128, 128, false, true, 4, EPI_ADD_SUMS)
+OB_GEMM_INSTANCE(64, 64, false, true, 8, EPI_ADD_SUMS)
 #undef OB_GEMM_INSTANCE
 template <class... A>
 constexpr size_t arg_bytes(void (*)(A...)) {
@@ -1199,33 +1208,36 @@ void launch_gemm_tn(int M, int N, int K, const void *A, int lda, const void *B, 
     launch_layout<true, true>(2, M, N, K, A, lda, B, N, C, N, nullptr, R, N, nullptr, s);
 }
 
-// An "NN" product whose contraction comes in pieces that are not in memory at one time: piece after piece leaves fp32 sums of all its tiles, like the
-// slices of a split contraction, and the last launch adds them in order.
+// An "NN" product whose contraction comes in pieces that are not in memory at one time: the first leaves fp32 sums of all its tiles, like the slices of a
+// split contraction, each after it adds its own to them, and a last launch rounds.
 template <int BM, int BN, int NS>
-static void nn_piece(int M, int N, int K, const void *A, int lda, const void *B, float *part, int index, hipStream_t s) {
+static void nn_piece(int M, int N, int K, const void *A, int lda, const void *B, float *part, bool first, hipStream_t s) {
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
-    const TailSplit ts{part + (size_t)index * tm * tn * (BM * BN), 0, tm * tn, 1, (K + KSTEP - 1) / KSTEP};
-    hipLaunchKernelGGL((gemm_kernel<BM, BN, 2, 2, false, true, NS>), dim3(tm * tn), dim3(256), 0, s, M, N, K, (const __bf16 *)A, lda,
-                       (const __bf16 *)B, N, (__bf16 *)nullptr, N, (const __bf16 *)nullptr, (const __bf16 *)nullptr, 0, tm, tn, ts);
+    const TailSplit ts{part, 0, tm * tn, 1, (K + KSTEP - 1) / KSTEP};
+#define OB_ARGS dim3(tm * tn), dim3(256), 0, s, M, N, K, (const __bf16 *)A, lda, (const __bf16 *)B, N, (__bf16 *)nullptr, N, (const __bf16 *)nullptr,  \
+                (const __bf16 *)nullptr, 0, tm, tn, ts
+    if (first) hipLaunchKernelGGL((gemm_kernel<BM, BN, 2, 2, false, true, NS>), OB_ARGS);
+    else hipLaunchKernelGGL((gemm_kernel<BM, BN, 2, 2, false, true, NS, EPI_ADD_SUMS>), OB_ARGS);
+#undef OB_ARGS
 }
 template <int BM, int BN>
-static void nn_sum(int M, int N, float *part, int pieces, void *C, hipStream_t s) {
+static void nn_round(int M, int N, float *part, void *C, hipStream_t s) {
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
-    const TailSplit ts{part, 0, tm * tn, pieces, 0};
+    const TailSplit ts{part, 0, tm * tn, 1, 0};
     hipLaunchKernelGGL((tail_sum_kernel<BM, BN>), dim3(tm * tn * (BM * BN / 8 / 256)), dim3(256), 0, s, ts, M, N, tm, tn,
                        (const __bf16 *)nullptr, (const __bf16 *)nullptr, 0, (__bf16 *)C, N, (const int32_t *)nullptr);
 }
-void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, int index, hipStream_t s) {
+void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, bool first, hipStream_t s) {
     ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
-    if (p.kind == BIG) nn_piece<256, 256, 4>(M, N, K, A, lda, B, part, index, s);
-    else if (p.kind == SMALL) nn_piece<128, 128, 4>(M, N, K, A, lda, B, part, index, s);
-    else nn_piece<64, 64, 8>(M, N, K, A, lda, B, part, index, s);
+    if (p.kind == BIG) nn_piece<256, 256, 4>(M, N, K, A, lda, B, part, first, s);
+    else if (p.kind == SMALL) nn_piece<128, 128, 4>(M, N, K, A, lda, B, part, first, s);
+    else nn_piece<64, 64, 8>(M, N, K, A, lda, B, part, first, s);
 }
-void launch_gemm_nn_sum(const Plan &p, int M, int N, float *part, int pieces, void *C, hipStream_t s) {
-    ProfScope prof(K_REDUCE, s, 4.0 * M * N * pieces + 2.0 * M * N);
-    if (p.kind == BIG) nn_sum<256, 256>(M, N, part, pieces, C, s);
-    else if (p.kind == SMALL) nn_sum<128, 128>(M, N, part, pieces, C, s);
-    else nn_sum<64, 64>(M, N, part, pieces, C, s);
+void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, hipStream_t s) {
+    ProfScope prof(K_REDUCE, s, 6.0 * M * N);
+    if (p.kind == BIG) nn_round<256, 256>(M, N, part, C, s);
+    else if (p.kind == SMALL) nn_round<128, 128>(M, N, part, C, s);
+    else nn_round<64, 64>(M, N, part, C, s);
 }
 
 }  // namespace ob

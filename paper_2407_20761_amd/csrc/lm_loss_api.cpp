@@ -45,7 +45,7 @@ Work work_layout(int n, int V, int H) {
     w.g = bwd.take((size_t)n * pc.ld * 2);
     if (pc.count > 1) {
         const Plan p = whole_plan(1, n, H, pc.cols);
-        w.sums_bytes = (size_t)pc.count * p.n_full * tile_rows(p.kind) * tile_cols(p.kind) * 4;
+        w.sums_bytes = (size_t)p.n_full * tile_rows(p.kind) * tile_cols(p.kind) * 4;
     } else {
         w.sums_bytes = gemm_workspace_bytes(1, n, H, V);
     }
@@ -72,16 +72,17 @@ bool aligned16(const void *p) { return (uintptr_t)p % 16 == 0; }
 int validate(const ob_lm_loss_desc *desc, const void *w, const void *x, int total_tokens, const int32_t *rows_host, const int32_t *rows_dev,
              int n_rows, const int32_t *labels, const void *ws, size_t ws_bytes, const char *who) {
     if (int rc = validate_desc(desc, who)) return rc;
-    if (!w || !x || !labels) return fail(OB_EINVAL, "%s: w / x / labels is null", who);
+    if (!w || !x || (n_rows && !labels)) return fail(OB_EINVAL, "%s: w / x / labels is null", who);
     if (total_tokens < 1 || total_tokens > MAX_TOKENS) return fail(OB_EINVAL, "%s: total_tokens %d outside [1, %d]", who, total_tokens, MAX_TOKENS);
-    if (n_rows < 1 || n_rows > total_tokens) return fail(OB_EINVAL, "%s: n_rows %d outside [1, total_tokens]", who, n_rows);
+    if (n_rows < 0 || n_rows > total_tokens) return fail(OB_EINVAL, "%s: n_rows %d outside [0, total_tokens]", who, n_rows);
+    if (!aligned16(w) || !aligned16(x)) return fail(OB_EINVAL, "%s: tensors must be aligned to 16 bytes", who);
+    if (n_rows == 0) return OB_OK;
     if (!rows_host != !rows_dev) return fail(OB_EINVAL, "%s: rows need a host and a device copy", who);
     if (!rows_host && n_rows != total_tokens) return fail(OB_EINVAL, "%s: without a row list n_rows is total_tokens", who);
     if (rows_host)
         for (int i = 0, last = -1; i < n_rows; last = rows_host[i++])
             if (rows_host[i] <= last || rows_host[i] >= total_tokens)
                 return fail(OB_EINVAL, "%s: rows[%d] = %d, must ascend inside [0, %d)", who, i, rows_host[i], total_tokens);
-    if (!aligned16(w) || !aligned16(x)) return fail(OB_EINVAL, "%s: tensors must be aligned to 16 bytes", who);
     if (!ws || !aligned16(ws) || ws_bytes < bytes_of(desc, n_rows))
         return fail(OB_EWORKSPACE, "%s: workspace too small (%zu bytes given) or not aligned", who, ws_bytes);
     return OB_OK;
@@ -99,6 +100,7 @@ extern "C" int ob_lm_loss_fwd(const ob_lm_loss_desc *desc, const void *w, const 
                               size_t ws_bytes, void *hip_stream) {
     const char *who = "ob_lm_loss_fwd";
     if (int rc = validate(desc, w, x, total_tokens, rows_host, rows_dev, n_rows, labels, ws, ws_bytes, who)) return rc;
+    if (n_rows == 0) return OB_OK;
     if (!nll || !lse) return fail(OB_EINVAL, "%s: nll / lse is null", who);
     hipStream_t s = (hipStream_t)hip_stream;
     const int n = n_rows, V = desc->vocab, H = desc->hidden;
@@ -125,10 +127,16 @@ extern "C" int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void
     const char *who = "ob_lm_loss_bwd";
     if (int rc = validate(desc, w, x, total_tokens, rows_host, rows_dev, n_rows, labels, ws, ws_bytes, who)) return rc;
     if (flags & ~OB_BWD_ACCUMULATE) return fail(OB_EINVAL, "%s: unknown flag bits %d", who, flags);
-    if (!lse || !dnll || !dx || !dw) return fail(OB_EINVAL, "%s: lse / dnll / dx / dw is null", who);
+    if ((n_rows && (!lse || !dnll)) || !dx || !dw) return fail(OB_EINVAL, "%s: lse / dnll / dx / dw is null", who);
     if (!aligned16(dx) || !aligned16(dw)) return fail(OB_EINVAL, "%s: tensors must be aligned to 16 bytes", who);
     hipStream_t s = (hipStream_t)hip_stream;
     const int n = n_rows, V = desc->vocab, H = desc->hidden, acc = flags & OB_BWD_ACCUMULATE;
+    if (n == 0) {
+        const int width = desc->dtype == OB_FP32 ? 2 * H : H;      // (rows of zeros, in elements of two bytes)
+        launch_rows_spread(nullptr, dx, nullptr, 0, total_tokens, width, s);
+        if (!acc) launch_rows_spread(nullptr, dw, nullptr, 0, V, width, s);
+        return check_launch(who);
+    }
     if (desc->dtype == OB_FP32) {
         f32::lm_loss_bwd(w, x, total_tokens, rows_dev, n, H, V, labels, lse, dnll, dx, dw, acc ? 1 : 0, ws, s);
         return check_launch(who);
@@ -153,10 +161,10 @@ extern "C" int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void
         unsigned char *dwp = (unsigned char *)dw + (size_t)v0 * H * 2;
         launch_loss_grad(whole_plan(0, n, cols, H), n, cols, H, xs, wp, labels, V, lse, dnll, v0, g, ld, s);
         launch_gemm_tn(cols, H, n, g, ld, xs, dwp, acc ? dwp : nullptr, s);
-        if (pc.count > 1) launch_gemm_nn_piece(p_dx, n, H, cols, g, ld, wp, sums, i, s);
+        if (pc.count > 1) launch_gemm_nn_piece(p_dx, n, H, cols, g, ld, wp, sums, i == 0, s);
         else launch_gemm_nn(n, H, cols, g, ld, wp, dxs, wk.sums_bytes ? sums : nullptr, wk.sums_bytes, s);
     }
-    if (pc.count > 1) launch_gemm_nn_sum(p_dx, n, H, sums, pc.count, dxs, s);
+    if (pc.count > 1) launch_gemm_nn_round(p_dx, n, H, sums, dxs, s);
     if (rows_dev) launch_rows_spread(dxs, dx, rows_dev, n, total_tokens, H, s);
     return check_launch(who);
 }

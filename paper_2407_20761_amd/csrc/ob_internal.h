@@ -67,9 +67,9 @@ void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, cons
 // C [M, N] = A [M, K] (row stride lda, zeros from K to a multiple of 64) B [K, N]; C = A [K, M]^T B [K, N] (+ R)
 void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *B, void *C, void *ws, size_t ws_bytes, hipStream_t s);
 void launch_gemm_tn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *R, hipStream_t s);
-// the first over pieces of K; part: `pieces` times whole tiles of p in fp32
-void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, int index, hipStream_t s);
-void launch_gemm_nn_sum(const Plan &p, int M, int N, float *part, int pieces, void *C, hipStream_t s);
+// the first over pieces of K; part: whole tiles of p in fp32
+void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, bool first, hipStream_t s);
+void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, hipStream_t s);
 // stats of `slots` parts of the vocabulary and the labels' logits -> lse, nll (0 for a row without a label)
 void launch_loss_combine(const void *stats, const float *target, const int32_t *labels, int n, int V, int slots, float *nll, float *lse,
                          hipStream_t s);

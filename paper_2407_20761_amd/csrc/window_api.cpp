@@ -1,6 +1,4 @@
 // C ABI of the varlen attention with a sliding window and sinks: validation, and the layout of the backward's workspace.
-#include <cmath>
-
 #include "attention_plan.h"
 #include "ob_internal.h"
 
@@ -15,7 +13,8 @@ int validate(const ob_segments *seg, int nq, int nkv, int d, int ldq, int ldkv, 
              const char *who) {
     if (int rc = validate_attn(seg, nq, nkv, d, ldq, ldkv, ldo, OB_MASK_SEG_CAUSAL, dtype, who)) return rc;
     if (ldq > MAX_STRIDE || ldkv > MAX_STRIDE || ldo > MAX_STRIDE) return fail(OB_EUNSUPPORTED, "%s: a row stride beyond %d elements", who, MAX_STRIDE);
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(OB_EINVAL, "%s: scale must be a positive number", who);
+    // (times the scale, the -1e30 of a masked score is to be far below every other, and finite)
+    if (!(scale >= 1e-20f && scale <= 1e6f)) return fail(OB_EINVAL, "%s: scale must lie in [1e-20, 1e6]", who);
     if (*window < 1) return fail(OB_EINVAL, "%s: window %d must be at least 1 (a row sees itself)", who, *window);
     if (sinks < 0) return fail(OB_EINVAL, "%s: sinks %d must not be negative", who, sinks);
     if (sinks > MAX_SINKS) return fail(OB_EUNSUPPORTED, "%s: sinks %d, at most %d", who, sinks, MAX_SINKS);

@@ -76,8 +76,7 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const float *__restrict
                                                          const int32_t *__restrict__ cu, int n_seg, int T, int nq, int group, float scale,
                                                          int window, int sinks) {
     constexpr int E = D / 16;
-    const long w = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (w >= (long)T * nq) return;
+    for (long w = (long)blockIdx.x * 4 + (threadIdx.x >> 6); w < (long)T * nq; w += (long)gridDim.x * 4) {
     const int t = (int)(w / nq), head = (int)(w % nq), lane = threadIdx.x & 63, mine = lane >> 4, col = (lane & 15) * E;
     const Keys keys(t, cu[segment_of(cu, n_seg, t)], window, sinks);
     const float *const kp = k + head / group * D + col, *const vp = v + head / group * D + col;
@@ -102,6 +101,7 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const float *__restrict
     for (int e = 0; e < E; ++e) ov.v[e] = across(ov.v[e] * f);
     if (mine == 0) ov.store(o + (size_t)t * ldo + head * D + col, 1.f / total);
     if (lane == 0) lse[(size_t)head * T + t] = top + logf(total);
+    }
 }
 
 // dq[t] = scale sum_j P_tj (dP_tj - delta_t) k_j; leaves delta_t = sum_d dO O for dK / dV
@@ -112,8 +112,7 @@ __global__ __launch_bounds__(256) void window_bwd_dq_kernel(const float *__restr
                                                             int ldq, int ldkv, int ldo, const int32_t *__restrict__ cu, int n_seg, int T, int nq,
                                                             int group, float scale, int window, int sinks) {
     constexpr int E = D / 16;
-    const long w = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (w >= (long)T * nq) return;
+    for (long w = (long)blockIdx.x * 4 + (threadIdx.x >> 6); w < (long)T * nq; w += (long)gridDim.x * 4) {
     const int t = (int)(w / nq), head = (int)(w % nq), lane = threadIdx.x & 63, mine = lane >> 4, col = (lane & 15) * E;
     const Keys keys(t, cu[segment_of(cu, n_seg, t)], window, sinks);
     const float *const kp = k + head / group * D + col, *const vp = v + head / group * D + col;
@@ -130,6 +129,7 @@ __global__ __launch_bounds__(256) void window_bwd_dq_kernel(const float *__restr
 #pragma unroll
     for (int e = 0; e < E; ++e) acc.v[e] = across(acc.v[e]);
     if (mine == 0) acc.store(dq + (size_t)t * ldq + head * D + col, scale);
+    }
 }
 
 // dk[j] = scale sum over the group's heads and the rows that see j of dS q; dv[j] = sum P dO: a workgroup to a key, sixteen rows at a time
@@ -141,7 +141,8 @@ __global__ __launch_bounds__(256) void window_bwd_dkv_kernel(const float *__rest
                                                              int group, float scale, int window, int sinks) {
     constexpr int E = D / 16;
     __shared__ float sums[4][2][D];
-    const int j = blockIdx.x / nkv, kvh = blockIdx.x % nkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (lane & 15) * E;
+    for (long w = blockIdx.x; w < (long)T * nkv; w += gridDim.x) {
+    const int j = (int)(w / nkv), kvh = (int)(w % nkv), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (lane & 15) * E;
     const int mine = threadIdx.x >> 4, seg = segment_of(cu, n_seg, j), start = cu[seg];
     const int end = j - start < sinks ? cu[seg + 1] : min(cu[seg + 1], j + window), rows = end - j;
     const Part<E> ke(k + (size_t)j * ldkv + kvh * D + col), ve(v + (size_t)j * ldkv + kvh * D + col);
@@ -169,9 +170,12 @@ __global__ __launch_bounds__(256) void window_bwd_dkv_kernel(const float *__rest
         float *const dst = (which ? dv : dk) + (size_t)j * ldkv + kvh * D + c;
         *dst = which ? s : s * scale;
     }
+    __syncthreads();
+    }
 }
 
-inline unsigned blocks_of(long rows) { return (unsigned)((rows + 3) / 4); }
+// (a launch has fewer than 2^32 threads: beyond, workgroups take several)
+inline unsigned blocks_of(long n) { return (unsigned)(n < (1 << 22) ? n : 1 << 22); }
 
 }  // namespace
 
@@ -184,7 +188,7 @@ inline unsigned blocks_of(long rows) { return (unsigned)((rows + 3) / 4); }
 void attn_window_fwd(const void *q, const void *k, const void *v, void *o, float *lse, int ldq, int ldkv, int ldo,
                      const ob_segments *seg, int nq, int nkv, int d, float scale, int window, int sinks, hipStream_t s) {
     const int T = seg->total_tokens;
-    OB_BY_SIZE(window_fwd_kernel, blocks_of((long)T * nq), (const float *)q, (const float *)k, (const float *)v, (float *)o, lse, ldq, ldkv, ldo,
+    OB_BY_SIZE(window_fwd_kernel, blocks_of(((long)T * nq + 3) / 4), (const float *)q, (const float *)k, (const float *)v, (float *)o, lse, ldq, ldkv, ldo,
                seg->cu_dev, seg->n_seg, T, nq, nq / nkv, scale, window, sinks);
 }
 
@@ -192,9 +196,9 @@ void attn_window_bwd(const void *d_o, const void *q, const void *k, const void *
                      void *dq, void *dk, void *dv, float *delta, int ldq, int ldkv, int ldo, const ob_segments *seg, int nq,
                      int nkv, int d, float scale, int window, int sinks, hipStream_t s) {
     const int T = seg->total_tokens;
-    OB_BY_SIZE(window_bwd_dq_kernel, blocks_of((long)T * nq), (const float *)d_o, (const float *)q, (const float *)k, (const float *)v,
+    OB_BY_SIZE(window_bwd_dq_kernel, blocks_of(((long)T * nq + 3) / 4), (const float *)d_o, (const float *)q, (const float *)k, (const float *)v,
                (const float *)o, lse, delta, (float *)dq, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, nq, nq / nkv, scale, window, sinks);
-    OB_BY_SIZE(window_bwd_dkv_kernel, (unsigned)((long)T * nkv), (const float *)d_o, (const float *)q, (const float *)k, (const float *)v, lse,
+    OB_BY_SIZE(window_bwd_dkv_kernel, blocks_of((long)T * nkv), (const float *)d_o, (const float *)q, (const float *)k, (const float *)v, lse,
                delta, (float *)dk, (float *)dv, ldq, ldkv, ldo, seg->cu_dev, seg->n_seg, T, nkv, nq / nkv, scale, window, sinks);
 }
 

@@ -161,6 +161,22 @@ def test_no_row_has_a_label(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_no_supervised_row(dtype):
+    c = Call(37, 64, 101, dtype=dtype)
+    none = ob.RowIndex(np.zeros(0, dtype=np.int32), device=DEV)
+    empty = torch.zeros(0, device=DEV)
+    assert ob.ob_lm_loss_workspace_bytes(c.desc, 0) == 0
+    ob.ob_lm_loss_fwd(c.desc, c.w, c.x, c.T, none, empty.int(), empty, empty, None)
+    ob.ob_lm_loss_bwd(c.desc, 0, c.w, c.x, c.T, none, empty.int(), empty, empty, c.dx, c.dw, None)
+    assert (c.dx == 0).all() and (c.dw == 0).all()
+    c.dx.fill_(float("nan"))
+    c.dw.fill_(3)
+    ob.ob_lm_loss_bwd(c.desc, ob.OB_BWD_ACCUMULATE, c.w, c.x, c.T, none, empty.int(), empty, empty, c.dx, c.dw, None)
+    assert (c.dx == 0).all() and (c.dw == 3).all()
+
+
+@gpu
 def test_large_logits():
     """logits of +-1000: the probabilities are 0 and 1, losses in the hundreds"""
     c = Call(130, 64, 3000, spread=300.0).run()
@@ -236,7 +252,7 @@ def _i32(values):
 @pytest.mark.parametrize("status,text,kw", [
     (3, "multiple of 64", {"H": 100}), (1, "dimension", {"H": 0}), (3, "hidden >", {"H": 8256}), (1, "dimension", {"V": 0}), (3, "vocab >", {"V": (1 << 21) + 1}),
     (1, "dtype", {"dtype": 3}), (1, "null", {"w": None}), (1, "null", {"labels": None}), (1, "null", {"lse": None}),
-    (1, "total_tokens", {"T": 0}), (1, "total_tokens", {"T": (1 << 22) + 1}), (1, "n_rows", {"n": 0}), (1, "n_rows", {"n": 11}),
+    (1, "total_tokens", {"T": 0}), (1, "total_tokens", {"T": (1 << 22) + 1}), (1, "n_rows", {"n": -1}), (1, "n_rows", {"n": 11}),
     (1, "host and a device", {"rows_dev": None}), (1, "rows[1] = 1", {"rows": (1, 1, 2)}), (1, "rows[2] = 10", {"rows": (1, 2, 10)}),
     (1, "rows[0] = -1", {"rows": (-1, 2, 3)}), (1, "rows[1] = 3", {"rows": (4, 3, 5)}), (1, "without a row list", {"rows": None, "rows_dev": None}),
     (1, "aligned", {"x": 0x1004}), (4, "workspace", {"ws": None}), (4, "workspace", {"ws_bytes": 16}), (4, "workspace", {"ws": 0x1008}),
@@ -267,5 +283,7 @@ def test_workspace_bytes():
     assert size(100, 10, 1) == 0 and size(64, 10, 0) == 0 and size(64, 10, (1 << 22) + 1) == 0
     # the gradient of the logits is kept within a piece: twice the vocabulary takes no second GiB, but for dx's sums and the maxima
     a, b = size(4096, 131072, 8192), size(4096, 262144, 8192)
-    assert 2 << 29 < a < b < a + (1 << 30)
+    assert 2 << 29 < a <= b < a + (1 << 29)
+    # nor do dx's sums grow with the pieces: 64 K rows take 16 of them, and 256 MB of sums for 1024 columns
+    assert size(1024, 131072, 65536) < (1 << 30) + 65536 * 1024 * (2 + 2 + 4) + (1 << 29)
     assert size(64, 1000, 100, 1) >= 100 * 1000 * 4

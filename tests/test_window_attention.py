@@ -255,6 +255,7 @@ def _refusal(status, text, fwd_only=False, **kw):
 @pytest.mark.parametrize("status,text,kw", [
     (1, "window 0", {"window": 0}), (1, "window -3", {"window": -3}), (1, "sinks -1", {"sinks": -1}), (3, "sinks 65", {"sinks": 65}),
     (1, "scale", {"scale": 0.0}), (1, "scale", {"scale": -1.0}), (1, "scale", {"scale": float("nan")}), (1, "scale", {"scale": float("inf")}),
+    (1, "scale", {"scale": 1e7}), (1, "scale", {"scale": 1e-21}),
     (3, "head_dim 96", {"d": 96}), (1, "multiple", {"nq": 3, "nkv": 2}), (1, "dtype", {"dtype": 2}), (1, "strides", {"ldq": 120}),
     (1, "strides", {"ldkv": 68}), (3, "stride", {"ldo": (1 << 24) + 8}), (2, "length", {"cu": (0, 5, 5)}), (1, "null", {"q": None}),
     (1, "null", {"lse": None}), (1, "aligned", {"k": 0x1008}), (4, "workspace", {"ws": None}), (4, "workspace", {"ws_bytes": 100}),
