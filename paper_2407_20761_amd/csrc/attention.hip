@@ -30,6 +30,7 @@ namespace ob {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
@@ -225,6 +226,22 @@ struct Tile {
 #endif
     }
 };
+
+// The probabilities of windowed dK / dV, times 2^P_LOG2, go from the role that forms them to the one that forms dS in fp16: 11 bits of each instead of
+// bf16's 8, so that dS is rounded once, as dQ's is (the gradients together 0.0026 off, 0.0024 so, 0.0017 of it their own rounding; from 2^-29 on a
+// probability keeps all 11 bits).  The factor is in the base-2 log-sum-exp that dQ leaves, and comes off with the sums.
+constexpr int P_LOG2 = 15;
+constexpr float P_OFF = 1.0f / (1 << P_LOG2);
+template <bool HALF>
+__device__ __forceinline__ float prob_of(const bf16x8 &p, int i) {
+    return HALF ? (float)__builtin_bit_cast(f16x8, p)[i] : (float)p[i];
+}
+__device__ __forceinline__ bf16x8 pack8_half(const f32x16 &a, int base) {
+    f16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = (_Float16)a[base + e];
+    return __builtin_bit_cast(bf16x8, o);
+}
 
 // accumulator registers 8 (u % 2) .. +7 of a 32x32 tile -> the 8-slot second operand of step u
 __device__ __forceinline__ bf16x8 pack8(const f32x16 &a, int base) {
@@ -780,7 +797,7 @@ __global__ __launch_bounds__(256, 2) void attn_bwd_dq_kernel(
     }
     dlt = sum_halves(dlt);
     if (q_live && lh == 0) {
-        lse2_all[(size_t)head * T + q_row] = lse2;
+        lse2_all[(size_t)head * T + q_row] = WIN::BAND ? lse2 - P_LOG2 : lse2;
         delta[(size_t)head * T + q_row] = dlt;
     }
     f32x16 acc_dq[DT];
@@ -898,9 +915,10 @@ __device__ __forceinline__ void dkv_scores(const unsigned char OB_LDS *__restric
 
 // role P: probabilities of the 32 MT x 32 score tile, packed as the second operands of the 2 MT
 // 16-row contraction steps (pk[mt][h] serves step 2 mt + h)
-template <bool CAUSAL, bool MASK, int MT>
+// (HALF: px, the same for the other role)
+template <bool CAUSAL, bool MASK, int MT, bool HALF>
 __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned char OB_LDS *__restrict__ lse2_s,
-                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2]) {
+                                          int q0, int seg_end, int kv_row, float sl2, bf16x8 (&pk)[MT][2], bf16x8 (&px)[MT][2]) {
     const int lh = (threadIdx.x & 63) >> 5;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -921,11 +939,13 @@ __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned 
         }
         pk[mt][0] = pack8(p, 0);
         pk[mt][1] = pack8(p, 8);
+        px[mt][0] = HALF ? pack8_half(p, 0) : pk[mt][0];
+        px[mt][1] = HALF ? pack8_half(p, 8) : pk[mt][1];
     }
 }
 
 // role G: dS = P (dP - Delta), in place of the packed probabilities
-template <int MT>
+template <int MT, bool HALF>
 __device__ __forceinline__ void dkv_dscores(const f32x16 (&dp)[MT], const unsigned char OB_LDS *__restrict__ dlt_s,
                                             bf16x8 (&pk)[MT][2]) {
     const int lh = (threadIdx.x & 63) >> 5;
@@ -938,7 +958,7 @@ __device__ __forceinline__ void dkv_dscores(const f32x16 (&dp)[MT], const unsign
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = 4 * g + e;
-                ds[r] = (float)pk[mt][r >> 3][r & 7] * (dp[mt][r] - d4[e]);
+                ds[r] = prob_of<HALF>(pk[mt][r >> 3], r & 7) * (dp[mt][r] - d4[e]);
             }
         }
         pk[mt][0] = pack8(ds, 0);
@@ -972,10 +992,11 @@ __device__ __forceinline__ void dkv_outputs(const unsigned char OB_LDS *__restri
 
 // role P: the products of dkv_outputs (probabilities pk of the tile before), the probabilities of the tile at hand between them:
 // two products, their operands read two products ahead, to 16 / D x 16 values per lane
-template <int D, int MT>
+template <int D, int MT, bool HALF>
 __device__ __forceinline__ void dkv_outputs_probs(const unsigned char OB_LDS *__restrict__ tile, const Tile<D, 32 * MT> &tl,
                                                   const bf16x8 (&pk)[MT][2], f32x16 (&acc_out)[D / 32], const f32x16 (&s)[MT],
-                                                  const unsigned char OB_LDS *__restrict__ lse2_s, float sl2, bf16x8 (&pn)[MT][2]) {
+                                                  const unsigned char OB_LDS *__restrict__ lse2_s, float sl2, bf16x8 (&pn)[MT][2],
+                                                  bf16x8 (&px)[MT][2]) {
     constexpr int DT = D / 32, PER = DT / 2, NB = 2 * MT * PER, EL = 8 / PER;      // batches of two products; values per lane and batch
     const int lh = (threadIdx.x & 63) >> 5;
     bf16x8 tf[2][2];
@@ -993,8 +1014,15 @@ __device__ __forceinline__ void dkv_outputs_probs(const unsigned char OB_LDS *__
         const int u = b / PER, e0 = (b % PER) * EL;
         if (b + 1 < NB) read(b + 1);
 #pragma unroll
-        for (int e = 0; e < EL; ++e)
-            pn[u >> 1][u & 1][e0 + e] = (__bf16)fast_exp2(s[u >> 1][8 * (u & 1) + e0 + e] * sl2 - l4[b & 1][e >> 2][e & 3]);
+        for (int e = 0; e < EL; ++e) {
+            const float p = fast_exp2(s[u >> 1][8 * (u & 1) + e0 + e] * sl2 - l4[b & 1][e >> 2][e & 3]);
+            pn[u >> 1][u & 1][e0 + e] = (__bf16)p;
+            if constexpr (HALF) {
+                f16x8 h = __builtin_bit_cast(f16x8, px[u >> 1][u & 1]);
+                h[e0 + e] = (_Float16)p;
+                px[u >> 1][u & 1] = __builtin_bit_cast(bf16x8, h);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int dt = 2 * (b % PER) + i;
@@ -1011,7 +1039,7 @@ __device__ __forceinline__ void dkv_outputs_probs(const unsigned char OB_LDS *__
 }
 
 // role G: the products of dkv_scores, dS = P (dP - Delta) of the tile before, in place of its probabilities pk, between them
-template <int D, int MT>
+template <int D, int MT, bool HALF>
 __device__ __forceinline__ void dkv_scores_dscores(const unsigned char OB_LDS *__restrict__ tile, const Tile<D, 32 * MT> &tl,
                                                    const bf16x8 (&held)[D / 16], f32x16 (&acc)[MT], const f32x16 (&dp)[MT],
                                                    const unsigned char OB_LDS *__restrict__ dlt_s, bf16x8 (&pk)[MT][2]) {
@@ -1037,7 +1065,7 @@ __device__ __forceinline__ void dkv_scores_dscores(const unsigned char OB_LDS *_
 #pragma unroll
         for (int e = 0; e < EL; ++e) {
             const int r = EL * b + e, mt = r >> 4;                          // accumulator register r % 16 of row tile mt
-            const float p = (float)pk[mt][(r >> 3) & 1][r & 7];
+            const float p = prob_of<HALF>(pk[mt][(r >> 3) & 1], r & 7);
             pk[mt][(r >> 3) & 1][r & 7] = (__bf16)(p * (dp[mt][r & 15] - d4[b & 1][e >> 2][e & 3]));
         }
 #pragma unroll
@@ -1344,6 +1372,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 && SR == 32 ? 2 : D == 128 || NP
         const bool late = !GEN || (RG ? live_prev : owed);
         if constexpr (!RG) {
             f32x16 acc_x[MT];
+            bf16x8 px[MT][2];
             if (live) {
                 if constexpr (MASK && WIN::BAND)
                     dkv_scores<D, MT, true>(tiles + S * BYTES, tl, kvf, acc_x, rows.hidden(kv_row, q0, 4 * lh));
@@ -1355,16 +1384,19 @@ __global__ __launch_bounds__(128 * NP, D == 128 && SR == 32 ? 2 : D == 128 || NP
             if (!GEN) request(NEXT);
             if constexpr (FUSE && !GEN) {
                 bf16x8 pn[MT][2];
-                dkv_outputs_probs<D, MT>(tiles + PREV * BYTES, tl, pk, acc_out, acc_x, stat + S * 256, sl2, pn);
+                dkv_outputs_probs<D, MT, HIDE>(tiles + PREV * BYTES, tl, pk, acc_out, acc_x, stat + S * 256, sl2, pn, px);
 #pragma unroll
-                for (int i = 0; i < 2 * MT; ++i) pk[i >> 1][i & 1] = pn[i >> 1][i & 1];
+                for (int i = 0; i < 2 * MT; ++i) {
+                    pk[i >> 1][i & 1] = pn[i >> 1][i & 1];
+                    if (!HIDE) px[i >> 1][i & 1] = pn[i >> 1][i & 1];
+                }
             } else {
                 if (FUSE && late) dkv_outputs<D, MT>(tiles + PREV * BYTES, tl, pk, acc_out);
-                if (live) dkv_probs<CAUSAL, MASK && !HIDE, MT>(acc_x, stat + S * 256, q0, ti.seg_end, kv_row, sl2, pk);
+                if (live) dkv_probs<CAUSAL, MASK && !HIDE, MT, HIDE>(acc_x, stat + S * 256, q0, ti.seg_end, kv_row, sl2, pk, px);
             }
             if (live) {
 #pragma unroll
-                for (int i = 0; i < 2 * MT; ++i) *(bf16x8 OB_LDS *)(p_new + i * 1024) = pk[i >> 1][i & 1];
+                for (int i = 0; i < 2 * MT; ++i) *(bf16x8 OB_LDS *)(p_new + i * 1024) = px[i >> 1][i & 1];
                 if (GEN || !FUSE) {
                     if (!owe) dkv_outputs<D, MT>(tiles + S * BYTES, tl, pk, acc_out);
                 }
@@ -1378,14 +1410,14 @@ __global__ __launch_bounds__(128 * NP, D == 128 && SR == 32 ? 2 : D == 128 || NP
             }
             if constexpr (FUSE && !GEN) {
                 f32x16 acc_x[MT];
-                dkv_scores_dscores<D, MT>(tiles + S * BYTES, tl, kvf, acc_x, dp_keep, stat + PREV * 256, pn);
+                dkv_scores_dscores<D, MT, HIDE>(tiles + S * BYTES, tl, kvf, acc_x, dp_keep, stat + PREV * 256, pn);
                 request(NEXT);
                 dkv_outputs<D, MT>(tiles + PREV * BYTES, tl, pn, acc_out);
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) dp_keep[mt] = acc_x[mt];
             } else {
                 if (late) {
-                    dkv_dscores<MT>(dp_keep, stat + PREV * 256, pn);
+                    dkv_dscores<MT, HIDE>(dp_keep, stat + PREV * 256, pn);
                     dkv_outputs<D, MT>(tiles + PREV * BYTES, tl, pn, acc_out);
                 }
                 if (!GEN) request(NEXT);
@@ -1434,7 +1466,7 @@ __global__ __launch_bounds__(128 * NP, D == 128 && SR == 32 ? 2 : D == 128 || NP
     if (rows.skip) return;
     if (!kv_live) return;
     // dV^T / dK^T of the whole group of query heads sit in the accumulators: one rounding to bf16
-    const float out_scale = role_g ? scale : 1.0f;
+    const float out_scale = HIDE ? (role_g ? scale : 1.0f) * P_OFF : role_g ? scale : 1.0f;
     __bf16 *const dst = role_g ? dk : dv;
     if (role_g && rot_log2_base > 0.f) rotary_bwd_row<D>(acc_out, kv_row - ti.seg_start, rot_log2_base, lh);
 #pragma unroll
@@ -1584,6 +1616,11 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 of[u] = lds16<bf16x8>(out_blk + (RG ? buf : buf ^ 1) * BUF + u * 1024);
+                if constexpr (WIN::BAND && !RG) {      // P as it lies there is what role G takes
+                    const bf16x8 half = of[u];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) of[u][e] = (__bf16)prob_of<true>(half, e);
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) tf[u][i] = Tile<D, SR>::frag_at(ot, tro[0][i], tro[1][i], u);
             }
@@ -1604,12 +1641,18 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
                 for (int e = 0; e < 8; ++e) {
                     const int r = 8 * h + e, g = r >> 2;
                     if constexpr (RG) {
-                        pk[h][e] = (__bf16)((float)pk[h][e] * (dp_keep[r] - row4[g][r & 3]));
+                        pk[h][e] = (__bf16)(prob_of<WIN::BAND>(pk[h], e) * (dp_keep[r] - row4[g][r & 3]));
                     } else {
                         const int qr = q0 + a * 32 + 8 * g + 4 * lh + (r & 3);
                         const bool ok = !MASK || WIN::BAND || (qr < ti.seg_end && (!CAUSAL || kv_row <= qr));
                         const float p = fast_exp2(s[r] * sl2 - row4[g][r & 3]);
-                        pk[h][e] = (__bf16)(ok ? p : 0.f);
+                        if constexpr (WIN::BAND) {
+                            f16x8 half = __builtin_bit_cast(f16x8, pk[h]);
+                            half[e] = (_Float16)p;
+                            pk[h] = __builtin_bit_cast(bf16x8, half);
+                        } else {
+                            pk[h][e] = (__bf16)(ok ? p : 0.f);
+                        }
                     }
                 }
             }
@@ -1652,7 +1695,7 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
     if (role_g) walk(std::true_type{}); else walk(std::false_type{});
     if (rows.skip) return;
     if (!kv_live) return;
-    const float out_scale = role_g ? scale : 1.0f;
+    const float out_scale = WIN::BAND ? (role_g ? scale : 1.0f) * P_OFF : role_g ? scale : 1.0f;
     __bf16 *const dst = role_g ? dk : dv;
     if (role_g && rot_log2_base > 0.f) rotary_bwd_pair<D>(acc_out[0], acc_out[1], a, kv_row - ti.seg_start, rot_log2_base, lh);
 #pragma unroll
@@ -1699,7 +1742,7 @@ __global__ __launch_bounds__(256) void attn_sink_sum_kernel(const float *__restr
     __syncthreads();
     if (wave != 0 || !live) return;
     sum = quarter[0][lane] + quarter[1][lane] + quarter[2][lane] + quarter[3][lane];
-    const float f = role ? scale : 1.f;
+    const float f = (role ? scale : 1.f) * P_OFF;
     bf16x4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = (__bf16)(sum[i] * f);
