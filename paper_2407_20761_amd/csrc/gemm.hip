@@ -717,7 +717,7 @@ __device__ __forceinline__ void gemm_tile(
                     const float p = __builtin_amdgcn_exp2f(z * LOG2E - lse2[r]) - (e == rel ? 1.f : 0.f);
                     g[e] = (__bf16)(weight[r] == 0.f || n_out + e >= N ? 0.f : p * weight[r]);
                 }
-                if (m < M && n_out < ldc) *(bf16x8 *)(Cm + (size_t)m * ldc + n_out) = g;
+                if (m < M && n_out < ldc) *(bf16x8 *)(Cm + (size_t)m * ldc + n_out) = g;      // (the next products read it: through the caches)
             }
         }
         return;
