@@ -243,6 +243,14 @@ __device__ __forceinline__ bf16x8 pack8_half(const f32x16 &a, int base) {
     return __builtin_bit_cast(bf16x8, o);
 }
 
+// for dV: rounded from fp16 in every launch shape, as one of them has nothing else in LDS
+__device__ __forceinline__ bf16x8 bf16_of_half(const bf16x8 &p) {
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = (__bf16)prob_of<true>(p, e);
+    return o;
+}
+
 // accumulator registers 8 (u % 2) .. +7 of a 32x32 tile -> the 8-slot second operand of step u
 __device__ __forceinline__ bf16x8 pack8(const f32x16 &a, int base) {
     bf16x8 o;
@@ -937,10 +945,16 @@ __device__ __forceinline__ void dkv_probs(const f32x16 (&s)[MT], const unsigned 
                 p[4 * g + e] = ok ? pe : 0.f;
             }
         }
-        pk[mt][0] = pack8(p, 0);
-        pk[mt][1] = pack8(p, 8);
-        px[mt][0] = HALF ? pack8_half(p, 0) : pk[mt][0];
-        px[mt][1] = HALF ? pack8_half(p, 8) : pk[mt][1];
+        if constexpr (HALF) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                px[mt][h] = pack8_half(p, 8 * h);
+                pk[mt][h] = bf16_of_half(px[mt][h]);
+            }
+        } else {
+            pk[mt][0] = px[mt][0] = pack8(p, 0);
+            pk[mt][1] = px[mt][1] = pack8(p, 8);
+        }
     }
 }
 
@@ -1016,11 +1030,14 @@ __device__ __forceinline__ void dkv_outputs_probs(const unsigned char OB_LDS *__
 #pragma unroll
         for (int e = 0; e < EL; ++e) {
             const float p = fast_exp2(s[u >> 1][8 * (u & 1) + e0 + e] * sl2 - l4[b & 1][e >> 2][e & 3]);
-            pn[u >> 1][u & 1][e0 + e] = (__bf16)p;
             if constexpr (HALF) {
+                const _Float16 half = (_Float16)p;
                 f16x8 h = __builtin_bit_cast(f16x8, px[u >> 1][u & 1]);
-                h[e0 + e] = (_Float16)p;
+                h[e0 + e] = half;
                 px[u >> 1][u & 1] = __builtin_bit_cast(bf16x8, h);
+                pn[u >> 1][u & 1][e0 + e] = (__bf16)(float)half;
+            } else {
+                pn[u >> 1][u & 1][e0 + e] = (__bf16)p;
             }
         }
 #pragma unroll
@@ -1616,11 +1633,7 @@ __global__ __launch_bounds__(512, 2) void attn_bwd_dkv_blocks_kernel(
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 of[u] = lds16<bf16x8>(out_blk + (RG ? buf : buf ^ 1) * BUF + u * 1024);
-                if constexpr (WIN::BAND && !RG) {      // P as it lies there is what role G takes
-                    const bf16x8 half = of[u];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) of[u][e] = (__bf16)prob_of<true>(half, e);
-                }
+                if constexpr (WIN::BAND && !RG) of[u] = bf16_of_half(of[u]);      // P as it lies there is what role G takes
 #pragma unroll
                 for (int i = 0; i < 2; ++i) tf[u][i] = Tile<D, SR>::frag_at(ot, tro[0][i], tro[1][i], u);
             }
