@@ -135,7 +135,8 @@ int ob_varlen_attn_bwd_static(const void *d_o, const void *q, const void *k, con
 /* ---- varlen attention with a sliding window and sinks ------------------------------------------
  * As above, causal, with allowed(i, j) <=> same segment, j <= i, and (i - j < window or j is one of the segment's first
  * `sinks` tokens).  window >= 1 (a row sees itself: none is empty; a window as long as the segments is plain causal
- * attention), 0 <= sinks <= 64, 1e-20 <= scale <= 1e6; row strides up to 2^24 elements, tensors and workspace aligned to 16 bytes.  Key
+ * attention), 0 <= sinks <= 64, 1e-20 <= scale <= 1e6, scores up to 2^20 in magnitude (beyond, fp32 sums do not tell
+ * probabilities); row strides up to 2^24 elements, tensors and workspace aligned to 16 bytes.  Key
  * tiles that no row of a workgroup sees are not computed, so a call costs tokens * window, not tokens^2.  Nothing of another segment is
  * read on a segment's behalf; inside a segment an infinity or NaN in a row of k, v or d_o may also reach rows near it that do not see it.
  * The backward's workspace (ob_varlen_attn_window_bwd_workspace_bytes for the same arguments; 0 if they are refused) holds the
@@ -274,7 +275,7 @@ int ob_connector_bwd(const ob_connector_desc *desc, const ob_connector_weights *
  * nll_r = lse_r - z_r,label, and for the gradients dnll_r of the losses
  *   G_rv = (exp(z_rv - lse_r) - [v = label_r]) dnll_r,   dx_r = sum_v G_rv W_v,   dW_v = sum_r G_rv x_r
  * The logits are never stored: the forward reduces each tile of them where it is computed, the backward computes them again
- * a piece of the vocabulary at a time (at most 1 GiB of G in bf16; dx is summed over the pieces in fp32, in order).  No
+ * a piece of the vocabulary at a time (at most 1 GiB of G in bf16, or 256 columns; dx is summed over the pieces in fp32, in order).  No
  * atomics: results are bitwise reproducible.
  * x [total_tokens, hidden], w [vocab, hidden].  rows (int32, n_rows entries, host and device copies): the supervised rows,
  * ascending, checked on the host; both NULL: every row (n_rows = total_tokens).  n_rows = 0 is a batch without a supervised
@@ -283,7 +284,8 @@ int ob_connector_bwd(const ob_connector_desc *desc, const ob_connector_weights *
  * outside [0, vocab) is ignored: nll 0, no gradient whatever its dnll (x of a listed row has to be finite).
  * ob_lm_loss_bwd, given lse of the forward, writes every row of dx (rows not listed: zeros) and dw (flags: OB_BWD_ACCUMULATE
  * adds to dw).  ws (ob_lm_loss_workspace_bytes) need not be kept between the two.  dtype OB_BF16, or OB_FP32 for the debug variant (x,
- * w, dx, dw fp32; plain kernels); hidden a multiple of 64 up to 8192, vocab up to 2^21, tensors and ws aligned to 16 bytes. */
+ * w, dx, dw fp32; plain kernels); hidden a multiple of 64 up to 8192, vocab up to 2^21, n_rows * vocab up to 2^39,
+ * tensors and ws aligned to 16 bytes. */
 typedef struct {
     int hidden, vocab;
     int dtype;         /* ob_dtype */

@@ -184,6 +184,13 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _ptr_i32(t):
+    """of a tensor of 32-bit whole numbers (labels, positions: torch makes them with 64 unless told otherwise)"""
+    if t is not None and t.dtype != torch.int32:
+        raise TypeError(f"expected int32, got {t.dtype}")
+    return _ptr(t)
+
+
 def _stream(stream=None):
     """the hipStream_t of a torch stream, of the current device's current one for None (asked for its raw handle: a
     torch.cuda.Stream object costs 2.7 us, a third of a small attention call)"""
@@ -317,7 +324,7 @@ class BlockAttn:
 
     def __init__(self, window=0, sinks=0, rotary=None, pos=None):
         self.rotary, self.pos = rotary, pos
-        self.c = ob_block_attn(int(window), int(sinks), None if rotary is None else C.pointer(rotary), _ptr(pos))
+        self.c = ob_block_attn(int(window), int(sinks), None if rotary is None else C.pointer(rotary), _ptr_i32(pos))
 
 
 def ob_block_attn_workspace_bytes(desc, attn: BlockAttn, seg: Segments) -> int:
@@ -456,12 +463,12 @@ def _row_list(rows, total_tokens):
 
 
 def ob_lm_loss_fwd(desc, w, x, total_tokens, rows: RowIndex | None, labels, nll, lse, ws, stream=None):
-    _check(lib.ob_lm_loss_fwd(C.byref(desc), _ptr(w), _ptr(x), total_tokens, *_row_list(rows, total_tokens), _ptr(labels), _ptr(nll), _ptr(lse),
+    _check(lib.ob_lm_loss_fwd(C.byref(desc), _ptr(w), _ptr(x), total_tokens, *_row_list(rows, total_tokens), _ptr_i32(labels), _ptr(nll), _ptr(lse),
                               _ptr(ws), _nbytes(ws), _stream(stream)))
 
 
 def ob_lm_loss_bwd(desc, flags, w, x, total_tokens, rows: RowIndex | None, labels, lse, dnll, dx, dw, ws, stream=None):
-    _check(lib.ob_lm_loss_bwd(C.byref(desc), int(flags), _ptr(w), _ptr(x), total_tokens, *_row_list(rows, total_tokens), _ptr(labels), _ptr(lse),
+    _check(lib.ob_lm_loss_bwd(C.byref(desc), int(flags), _ptr(w), _ptr(x), total_tokens, *_row_list(rows, total_tokens), _ptr_i32(labels), _ptr(lse),
                               _ptr(dnll), _ptr(dx), _ptr(dw), _ptr(ws), _nbytes(ws), _stream(stream)))
 
 
@@ -470,11 +477,13 @@ def make_rotary_axes_desc(axis_of_pair, head_dim, base=10000.0, per_axis=False) 
     axes = [int(a) for a in axis_of_pair]
     if len(axes) != head_dim // 2 or not 1 <= len(axes) <= 64:
         raise ValueError(f"{len(axes)} pairs given, a head of {head_dim} has {head_dim // 2} (at most 64)")
+    if not all(-1 <= a < 127 for a in axes):
+        raise ValueError(f"axes {axes}: -1 for a pair that passes, else from 0 on")
     return ob_rotary_axes_desc(int(head_dim), max(0, *axes) + 1, float(base), int(bool(per_axis)), (C.c_int8 * 64)(*axes))
 
 
 def ob_rotary_axes(desc, x, ldx, y, ldy, total_tokens, n_heads, pos, inverse=False, dtype=OB_BF16, stream=None):
-    _check(lib.ob_rotary_axes(C.byref(desc), _ptr(x), ldx, _ptr(y), ldy, total_tokens, n_heads, _ptr(pos), int(bool(inverse)), dtype,
+    _check(lib.ob_rotary_axes(C.byref(desc), _ptr(x), ldx, _ptr(y), ldy, total_tokens, n_heads, _ptr_i32(pos), int(bool(inverse)), dtype,
                               _stream(stream)))
 
 

@@ -611,7 +611,7 @@ __global__ __launch_bounds__(256) void loss_gemm_kernel(int M, int N, int K, con
     typedef __attribute__((ext_vector_type(16))) float f32x16;
     __shared__ float sums[4][32][33];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = lane & 31, h = lane >> 5;
-    const int tiles_m = (M + 31) / 32, m0 = blockIdx.x % tiles_m * 32, n0 = blockIdx.x / tiles_m * 32;
+    const int m0 = (AK && BK ? blockIdx.y : blockIdx.x) * 32, n0 = (AK && BK ? blockIdx.x : blockIdx.y) * 32;      // (the vocabulary's in x, which may be long)
     const long m = min(m0 + x, M - 1), n = min(n0 + x, N - 1);
     auto load = [](const float *p, long row, long ld, int k, bool inner) {
         f32x4 v;
@@ -654,7 +654,8 @@ __global__ __launch_bounds__(256) void loss_gemm_kernel(int M, int N, int K, con
     }
 }
 static void loss_gemm(int layout, int M, int N, int K, const float *A, const float *B, float *C, int accumulate, hipStream_t s) {
-    const dim3 grid((unsigned)((M + 31) / 32) * ((N + 31) / 32));
+    const unsigned tm = (M + 31) / 32, tn = (N + 31) / 32;
+    const dim3 grid(layout == 0 ? tn : tm, layout == 0 ? tm : tn);
     if (layout == 0) hipLaunchKernelGGL((loss_gemm_kernel<true, true>), grid, dim3(256), 0, s, M, N, K, A, K, B, K, C, accumulate);
     else if (layout == 1) hipLaunchKernelGGL((loss_gemm_kernel<true, false>), grid, dim3(256), 0, s, M, N, K, A, K, B, N, C, accumulate);
     else hipLaunchKernelGGL((loss_gemm_kernel<false, false>), grid, dim3(256), 0, s, M, N, K, A, M, B, N, C, accumulate);
@@ -703,29 +704,29 @@ struct LossWork { size_t xs, dxs, z, total; int rows; };
 static LossWork loss_work(int n, int H, int V) {
     LossWork w; size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += up256(bytes); return o; };
-    const int fit = (1 << 24) / V;      // 64 MB of logits
-    w.rows = fit < 1 ? 1 : fit < n ? fit : n;
-    w.xs = take((size_t)n * H * 4); w.dxs = take((size_t)n * H * 4); w.z = take((size_t)w.rows * V * 4);
+    const int fit = V < 256 ? 1 << 16 : (1 << 24) / V;      // 64 MB of logits, and less than 2^32 threads to copy the rows
+    w.rows = fit < n ? fit : n;
+    w.xs = take((size_t)w.rows * H * 4); w.dxs = take((size_t)n * H * 4); w.z = take((size_t)w.rows * V * 4);
     w.total = off;
     return w;
 }
 size_t lm_loss_work_bytes(int n, int H, int V) { return loss_work(n, H, V).total; }
 
-static const float *loss_rows(const void *x, const int32_t *rows_dev, int n, int H, const LossWork &wk, unsigned char *ws, hipStream_t s) {
-    if (!rows_dev) return OB_F(x);
-    hipLaunchKernelGGL(rows_copy_kernel, dim3(blocks_for((long)n * H)), dim3(256), 0, s, OB_FM(ws + wk.xs), (float *)x /* read only */, rows_dev,
-                       (long)n * H, H, 0);
+// rows i .. i + m of the list
+static const float *loss_rows(const void *x, const int32_t *rows_dev, int i, int m, int H, const LossWork &wk, unsigned char *ws, hipStream_t s) {
+    if (!rows_dev) return OB_F(x) + (size_t)i * H;
+    hipLaunchKernelGGL(rows_copy_kernel, dim3(blocks_for((long)m * H)), dim3(256), 0, s, OB_FM(ws + wk.xs), (float *)x /* read only */, rows_dev + i,
+                       (long)m * H, H, 0);
     return OB_F(ws + wk.xs);
 }
 
 void lm_loss_fwd(const void *w, const void *x, const int32_t *rows_dev, int n, int H, int V, const int32_t *labels, float *nll, float *lse,
                  void *ws, hipStream_t s) {
     const LossWork wk = loss_work(n, H, V);
-    const float *xs = loss_rows(x, rows_dev, n, H, wk, (unsigned char *)ws, s);
     float *z = OB_FM((unsigned char *)ws + wk.z);
     for (int i = 0; i < n; i += wk.rows) {
         const int m = n - i < wk.rows ? n - i : wk.rows;
-        loss_gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, 0, s);
+        loss_gemm(0, m, V, H, loss_rows(x, rows_dev, i, m, H, wk, (unsigned char *)ws, s), OB_F(w), z, 0, s);
         hipLaunchKernelGGL((loss_row_kernel<false>), dim3(m), dim3(256), 0, s, z, V, labels + i, nll + i, lse + i, (const float *)nullptr);
     }
 }
@@ -734,14 +735,14 @@ void lm_loss_bwd(const void *w, const void *x, int T, const int32_t *rows_dev, i
                  const float *dnll, void *dx, void *dw, int accumulate, void *ws, hipStream_t s) {
     const LossWork wk = loss_work(n, H, V);
     unsigned char *wb = (unsigned char *)ws;
-    const float *xs = loss_rows(x, rows_dev, n, H, wk, wb, s);
     float *z = OB_FM(wb + wk.z), *dxs = rows_dev ? OB_FM(wb + wk.dxs) : OB_FM(dx);
     for (int i = 0; i < n; i += wk.rows) {
         const int m = n - i < wk.rows ? n - i : wk.rows;
-        loss_gemm(0, m, V, H, xs + (size_t)i * H, OB_F(w), z, 0, s);
+        const float *xs = loss_rows(x, rows_dev, i, m, H, wk, wb, s);
+        loss_gemm(0, m, V, H, xs, OB_F(w), z, 0, s);
         hipLaunchKernelGGL((loss_row_kernel<true>), dim3(m), dim3(256), 0, s, z, V, labels + i, (float *)nullptr, (float *)lse + i /* read only */,
                            dnll + i);
-        loss_gemm(2, V, H, m, z, xs + (size_t)i * H, OB_FM(dw), accumulate || i > 0 ? 1 : 0, s);
+        loss_gemm(2, V, H, m, z, xs, OB_FM(dw), accumulate || i > 0 ? 1 : 0, s);
         loss_gemm(1, m, H, V, z, OB_F(w), dxs + (size_t)i * H, 0, s);
     }
     if (rows_dev) hipLaunchKernelGGL(rows_spread_kernel, dim3(T), dim3(256), 0, s, dxs, OB_FM(dx), rows_dev, n, H);

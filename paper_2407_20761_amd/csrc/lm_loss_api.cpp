@@ -8,7 +8,9 @@ using namespace ob;
 namespace {
 
 constexpr int MAX_HIDDEN = 8192, MAX_VOCAB = 1 << 21;
-// Bytes that the gradient of the logits, in bf16, may take at a time
+// a launch has fewer than 2^32 threads, 256 to a tile of 256 x 256 logits
+constexpr long MAX_LOGITS = 1l << 39;
+// Bytes that the gradient of the logits, in bf16, may take at a time (256 columns, if they are more)
 constexpr size_t PIECE_BYTES = (size_t)1 << 30;
 
 struct Bump {
@@ -77,6 +79,7 @@ int validate(const ob_lm_loss_desc *desc, const void *w, const void *x, int tota
     if (n_rows < 0 || n_rows > total_tokens) return fail(OB_EINVAL, "%s: n_rows %d outside [0, total_tokens]", who, n_rows);
     if (!aligned16(w) || !aligned16(x)) return fail(OB_EINVAL, "%s: tensors must be aligned to 16 bytes", who);
     if (n_rows == 0) return OB_OK;
+    if ((long)n_rows * desc->vocab > MAX_LOGITS) return fail(OB_EUNSUPPORTED, "%s: n_rows x vocab beyond 2^39", who);
     if (!rows_host != !rows_dev) return fail(OB_EINVAL, "%s: rows need a host and a device copy", who);
     if (!rows_host && n_rows != total_tokens) return fail(OB_EINVAL, "%s: without a row list n_rows is total_tokens", who);
     if (rows_host)
@@ -91,7 +94,8 @@ int validate(const ob_lm_loss_desc *desc, const void *w, const void *x, int tota
 }  // namespace
 
 extern "C" size_t ob_lm_loss_workspace_bytes(const ob_lm_loss_desc *desc, int n_rows) {
-    if (validate_desc(desc, "ob_lm_loss_workspace_bytes") || n_rows < 1 || n_rows > MAX_TOKENS) return 0;
+    if (validate_desc(desc, "ob_lm_loss_workspace_bytes") || n_rows < 1 || n_rows > MAX_TOKENS || (long)n_rows * desc->vocab > MAX_LOGITS)
+        return 0;
     return bytes_of(desc, n_rows);
 }
 

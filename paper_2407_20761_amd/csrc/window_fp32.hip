@@ -77,30 +77,30 @@ __global__ __launch_bounds__(256) void window_fwd_kernel(const float *__restrict
                                                          int window, int sinks) {
     constexpr int E = D / 16;
     for (long w = (long)blockIdx.x * 4 + (threadIdx.x >> 6); w < (long)T * nq; w += (long)gridDim.x * 4) {
-    const int t = (int)(w / nq), head = (int)(w % nq), lane = threadIdx.x & 63, mine = lane >> 4, col = (lane & 15) * E;
-    const Keys keys(t, cu[segment_of(cu, n_seg, t)], window, sinks);
-    const float *const kp = k + head / group * D + col, *const vp = v + head / group * D + col;
-    const Part<E> qv(q + (size_t)t * ldq + head * D + col);
-    Part<E> ov;
-    float m = -INFINITY, l = 0.f;
-    for (int i = mine; i < (keys.n + 3) / 4 * 4; i += 4) {          // (all four groups as often: they exchange)
-        const size_t row = (size_t)keys.at(min(i, keys.n - 1)) * ldkv;
-        const Part<E> ke(kp + row), ve(vp + row);
-        const float dot = qv.dot(ke);
-        if (i >= keys.n) continue;
-        const float s = dot * scale, mn = fmaxf(m, s), alpha = expf(m - mn), p = expf(s - mn);
-        l = l * alpha + p;
+        const int t = (int)(w / nq), head = (int)(w % nq), lane = threadIdx.x & 63, mine = lane >> 4, col = (lane & 15) * E;
+        const Keys keys(t, cu[segment_of(cu, n_seg, t)], window, sinks);
+        const float *const kp = k + head / group * D + col, *const vp = v + head / group * D + col;
+        const Part<E> qv(q + (size_t)t * ldq + head * D + col);
+        Part<E> ov;
+        float m = -INFINITY, l = 0.f;
+        for (int i = mine; i < (keys.n + 3) / 4 * 4; i += 4) {          // (all four groups as often: they exchange)
+            const size_t row = (size_t)keys.at(min(i, keys.n - 1)) * ldkv;
+            const Part<E> ke(kp + row), ve(vp + row);
+            const float dot = qv.dot(ke);
+            if (i >= keys.n) continue;
+            const float s = dot * scale, mn = fmaxf(m, s), alpha = expf(m - mn), p = expf(s - mn);
+            l = l * alpha + p;
 #pragma unroll
-        for (int e = 0; e < E; ++e) ov.v[e] = ov.v[e] * alpha + p * ve.v[e];
-        m = mn;
-    }
-    const float top = fmaxf(fmaxf(m, __shfl_xor(m, 16)), fmaxf(__shfl_xor(m, 32), __shfl_xor(m, 48)));
-    const float f = m == -INFINITY ? 0.f : expf(m - top);           // (a group without a key)
-    const float total = across(l * f);
+            for (int e = 0; e < E; ++e) ov.v[e] = ov.v[e] * alpha + p * ve.v[e];
+            m = mn;
+        }
+        const float top = fmaxf(fmaxf(m, __shfl_xor(m, 16)), fmaxf(__shfl_xor(m, 32), __shfl_xor(m, 48)));
+        const float f = m == -INFINITY ? 0.f : expf(m - top);           // (a group without a key)
+        const float total = across(l * f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) ov.v[e] = across(ov.v[e] * f);
-    if (mine == 0) ov.store(o + (size_t)t * ldo + head * D + col, 1.f / total);
-    if (lane == 0) lse[(size_t)head * T + t] = top + logf(total);
+        for (int e = 0; e < E; ++e) ov.v[e] = across(ov.v[e] * f);
+        if (mine == 0) ov.store(o + (size_t)t * ldo + head * D + col, 1.f / total);
+        if (lane == 0) lse[(size_t)head * T + t] = top + logf(total);
     }
 }
 
@@ -113,22 +113,22 @@ __global__ __launch_bounds__(256) void window_bwd_dq_kernel(const float *__restr
                                                             int group, float scale, int window, int sinks) {
     constexpr int E = D / 16;
     for (long w = (long)blockIdx.x * 4 + (threadIdx.x >> 6); w < (long)T * nq; w += (long)gridDim.x * 4) {
-    const int t = (int)(w / nq), head = (int)(w % nq), lane = threadIdx.x & 63, mine = lane >> 4, col = (lane & 15) * E;
-    const Keys keys(t, cu[segment_of(cu, n_seg, t)], window, sinks);
-    const float *const kp = k + head / group * D + col, *const vp = v + head / group * D + col;
-    const Part<E> qv(q + (size_t)t * ldq + head * D + col), go(d_o + (size_t)t * ldo + head * D + col), ov(o + (size_t)t * ldo + head * D + col);
-    const float ls = lse[(size_t)head * T + t], dl = go.dot(ov);
-    if (lane == 0) delta[(size_t)head * T + t] = dl;
-    Part<E> acc;
-    for (int i = mine; i < (keys.n + 3) / 4 * 4; i += 4) {
-        const size_t row = (size_t)keys.at(min(i, keys.n - 1)) * ldkv;
-        const Part<E> ke(kp + row), ve(vp + row);
-        const float s = qv.dot(ke), dp = go.dot(ve);
-        if (i < keys.n) acc.add(expf(s * scale - ls) * (dp - dl), ke);
-    }
+        const int t = (int)(w / nq), head = (int)(w % nq), lane = threadIdx.x & 63, mine = lane >> 4, col = (lane & 15) * E;
+        const Keys keys(t, cu[segment_of(cu, n_seg, t)], window, sinks);
+        const float *const kp = k + head / group * D + col, *const vp = v + head / group * D + col;
+        const Part<E> qv(q + (size_t)t * ldq + head * D + col), go(d_o + (size_t)t * ldo + head * D + col), ov(o + (size_t)t * ldo + head * D + col);
+        const float ls = lse[(size_t)head * T + t], dl = go.dot(ov);
+        if (lane == 0) delta[(size_t)head * T + t] = dl;
+        Part<E> acc;
+        for (int i = mine; i < (keys.n + 3) / 4 * 4; i += 4) {
+            const size_t row = (size_t)keys.at(min(i, keys.n - 1)) * ldkv;
+            const Part<E> ke(kp + row), ve(vp + row);
+            const float s = qv.dot(ke), dp = go.dot(ve);
+            if (i < keys.n) acc.add(expf(s * scale - ls) * (dp - dl), ke);
+        }
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc.v[e] = across(acc.v[e]);
-    if (mine == 0) acc.store(dq + (size_t)t * ldq + head * D + col, scale);
+        for (int e = 0; e < E; ++e) acc.v[e] = across(acc.v[e]);
+        if (mine == 0) acc.store(dq + (size_t)t * ldq + head * D + col, scale);
     }
 }
 
@@ -142,35 +142,35 @@ __global__ __launch_bounds__(256) void window_bwd_dkv_kernel(const float *__rest
     constexpr int E = D / 16;
     __shared__ float sums[4][2][D];
     for (long w = blockIdx.x; w < (long)T * nkv; w += gridDim.x) {
-    const int j = (int)(w / nkv), kvh = (int)(w % nkv), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (lane & 15) * E;
-    const int mine = threadIdx.x >> 4, seg = segment_of(cu, n_seg, j), start = cu[seg];
-    const int end = j - start < sinks ? cu[seg + 1] : min(cu[seg + 1], j + window), rows = end - j;
-    const Part<E> ke(k + (size_t)j * ldkv + kvh * D + col), ve(v + (size_t)j * ldkv + kvh * D + col);
-    Part<E> ak, av;
-    for (int head = kvh * group; head < (kvh + 1) * group; ++head)
-        for (int i = mine; i < (rows + 15) / 16 * 16; i += 16) {
-            const int t = j + min(i, rows - 1);
-            const Part<E> qe(q + (size_t)t * ldq + head * D + col), ge(d_o + (size_t)t * ldo + head * D + col);
-            const float ls = lse[(size_t)head * T + t], dl = delta[(size_t)head * T + t];
-            const float s = qe.dot(ke), dp = ge.dot(ve);
-            if (i >= rows) continue;
-            const float p = expf(s * scale - ls);
-            av.add(p, ge);
-            ak.add(p * (dp - dl), qe);
-        }
+        const int j = (int)(w / nkv), kvh = (int)(w % nkv), lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = (lane & 15) * E;
+        const int mine = threadIdx.x >> 4, seg = segment_of(cu, n_seg, j), start = cu[seg];
+        const int end = j - start < sinks ? cu[seg + 1] : min(cu[seg + 1], j + window), rows = end - j;
+        const Part<E> ke(k + (size_t)j * ldkv + kvh * D + col), ve(v + (size_t)j * ldkv + kvh * D + col);
+        Part<E> ak, av;
+        for (int head = kvh * group; head < (kvh + 1) * group; ++head)
+            for (int i = mine; i < (rows + 15) / 16 * 16; i += 16) {
+                const int t = j + min(i, rows - 1);
+                const Part<E> qe(q + (size_t)t * ldq + head * D + col), ge(d_o + (size_t)t * ldo + head * D + col);
+                const float ls = lse[(size_t)head * T + t], dl = delta[(size_t)head * T + t];
+                const float s = qe.dot(ke), dp = ge.dot(ve);
+                if (i >= rows) continue;
+                const float p = expf(s * scale - ls);
+                av.add(p, ge);
+                ak.add(p * (dp - dl), qe);
+            }
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const float a = across(ak.v[e]), b = across(av.v[e]);
-        if (lane < 16) { sums[wave][0][col + e] = a; sums[wave][1][col + e] = b; }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2 * D; i += 256) {
-        const int which = i / D, c = i % D;
-        const float s = sums[0][which][c] + sums[1][which][c] + sums[2][which][c] + sums[3][which][c];
-        float *const dst = (which ? dv : dk) + (size_t)j * ldkv + kvh * D + c;
-        *dst = which ? s : s * scale;
-    }
-    __syncthreads();
+        for (int e = 0; e < E; ++e) {
+            const float a = across(ak.v[e]), b = across(av.v[e]);
+            if (lane < 16) { sums[wave][0][col + e] = a; sums[wave][1][col + e] = b; }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * D; i += 256) {
+            const int which = i / D, c = i % D;
+            const float s = sums[0][which][c] + sums[1][which][c] + sums[2][which][c] + sums[3][which][c];
+            float *const dst = (which ? dv : dk) + (size_t)j * ldkv + kvh * D + c;
+            *dst = which ? s : s * scale;
+        }
+        __syncthreads();
     }
 }
 

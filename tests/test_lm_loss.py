@@ -110,7 +110,8 @@ def test_some_rows(T, n, H, V):
 
 
 @gpu
-@pytest.mark.parametrize("T,n,H,V", [(5, 5, 64, 3), (130, 70, 128, 1009), (600, 600, 64, 40001)])
+@pytest.mark.parametrize("T,n,H,V", [(5, 5, 64, 3), (130, 70, 128, 1009), (600, 600, 64, 40001),
+                                     (70000, 66000, 64, 3), (3, 2, 64, 600000)])
 def test_fp32(T, n, H, V):
     Call(T, H, V, rows=None if n == T else _some_rows(T, n), dtype=torch.float32).run().check()
 
@@ -245,6 +246,16 @@ def test_side_stream_and_captured_calls():
 
 # ---- refusals: no GPU ------------------------------------------------------------------------------
 
+def test_labels_of_64_bits():
+    """which torch makes unless told otherwise, and the kernels would read as pairs"""
+    x, labels, f = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int64), torch.zeros(4)
+    desc = ob.make_lm_loss_desc(64, 4)
+    with pytest.raises(TypeError, match="int32"):
+        ob.ob_lm_loss_fwd(desc, x, x, 4, None, labels, f, f, x, x)
+    with pytest.raises(TypeError, match="int32"):
+        ob.ob_lm_loss_bwd(desc, 0, x, x, 4, None, labels, f, f, x, x, x, x)
+
+
 def _i32(values):
     return (C.c_int32 * max(len(values), 1))(*values)
 
@@ -256,6 +267,7 @@ def _i32(values):
     (1, "host and a device", {"rows_dev": None}), (1, "rows[1] = 1", {"rows": (1, 1, 2)}), (1, "rows[2] = 10", {"rows": (1, 2, 10)}),
     (1, "rows[0] = -1", {"rows": (-1, 2, 3)}), (1, "rows[1] = 3", {"rows": (4, 3, 5)}), (1, "without a row list", {"rows": None, "rows_dev": None}),
     (1, "aligned", {"x": 0x1004}), (4, "workspace", {"ws": None}), (4, "workspace", {"ws_bytes": 16}), (4, "workspace", {"ws": 0x1008}),
+    (3, "2^39", {"T": 1 << 22, "n": 1 << 22, "V": (1 << 17) + 1}),
 ])
 def test_refusals(status, text, kw):
     a = dict(H=128, V=1000, dtype=0, w=0x1000, x=0x1000, T=10, rows=(1, 4, 7), rows_dev=0x1000, n=3, labels=0x1000, nll=0x1000, lse=0x1000,
@@ -280,6 +292,7 @@ def test_refusals_of_the_backward():
 
 def test_workspace_bytes():
     size = lambda H, V, n, dtype=0: ob.ob_lm_loss_workspace_bytes(ob.make_lm_loss_desc(H, V, dtype), n)
+    assert size(64, (1 << 17) + 1, 1 << 22) == 0 and size(64, 1 << 17, 1 << 22) > 0
     assert size(100, 10, 1) == 0 and size(64, 10, 0) == 0 and size(64, 10, (1 << 22) + 1) == 0
     # the gradient of the logits is kept within a piece: twice the vocabulary takes no second GiB, but for dx's sums and the maxima
     a, b = size(4096, 131072, 8192), size(4096, 262144, 8192)
@@ -287,3 +300,6 @@ def test_workspace_bytes():
     # nor do dx's sums grow with the pieces: 64 K rows take 16 of them, and 256 MB of sums for 1024 columns
     assert size(1024, 131072, 65536) < (1 << 30) + 65536 * 1024 * (2 + 2 + 4) + (1 << 29)
     assert size(64, 1000, 100, 1) >= 100 * 1000 * 4
+    # fp32: 64 MB of logits at a time, dx's rows and no more than 64 K rows of x
+    assert size(8192, 1, 1 << 22, 1) <= ((1 << 22) + (1 << 16)) * 8192 * 4 + (1 << 26) + 1024
+    assert size(64, 1 << 21, 1 << 18, 1) <= (1 << 18) * 64 * 4 + (1 << 26) + (1 << 12)

@@ -167,4 +167,15 @@ def test_make_desc_counts_the_pairs():
         ob.make_rotary_axes_desc([0] * 31, 64)
     with pytest.raises(ValueError):
         ob.make_rotary_axes_desc([0] * 100, 200)
+    for axis in (-2, -257, 127, 256):      # (the description holds 8 bits of it)
+        with pytest.raises(ValueError):
+            ob.make_rotary_axes_desc([axis] + [0] * 31, 64)
     assert ob.make_rotary_axes_desc([-1] * 32, 64).n_axes == 1
+
+
+def test_positions_of_64_bits():
+    x, pos, desc = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros((1, 4), dtype=torch.int64), ob.make_rotary_axes_desc([0] * 32, 64)
+    with pytest.raises(TypeError, match="int32"):
+        ob.ob_rotary_axes(desc, x, 64, x, 64, 4, 1, pos)
+    with pytest.raises(TypeError, match="int32"):
+        ob.BlockAttn(rotary=desc, pos=pos)
