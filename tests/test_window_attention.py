@@ -116,6 +116,18 @@ def test_fp32(lens, nq, nkv, d, window, sinks):
 
 @gpu
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(2, 0), (3, 1), (12, 0)])
+def test_rows_of_few_keys(d, window, sinks):
+    """A rounding's error is at most U of the value, spread evenly: U / sqrt(3) in the mean square.  Of dS and of the result that is
+    sqrt(2 / 3) U in norm; a Delta from the rounded o alone would be off by more than that at two keys to a row"""
+    c = _call([500, 1, 130], 4, 2, d, window, sinks).run()
+    got, want = c.results(), c.expected()
+    for n in ("dq", "dk", "dv"):
+        assert np.linalg.norm(got[n] - want[n][0]) <= (2 / 3) ** 0.5 * U * np.linalg.norm(want[n][0]), n
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
 def test_many_segments(d):
     """more segments than the search for a tile looks at in a round, and more tiles than the table of the order of work holds"""
     rng = np.random.default_rng(5)
