@@ -532,7 +532,7 @@ struct KLoop {
 // The last two are those of the cross entropy over a vocabulary, whose logits z = x W^T ("NT") are not stored:
 //   EPI_LOSS_STATS  per row of z and column half of a tile its maximum and the sum of exp(z - maximum): float2 [2 tiles_n][M] in place of C; the logit of
 //                   the row's label (in place of R) to float [M] in place of the bias, by the lane that holds it
-//   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) dnll, zeros in the columns N .. ldc; labels in place of R, dnll of the bias, lse of the slice
+//   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) dnll, zeros in the columns N .. ldc, rounded once, to bf16: the operand of two products; labels in place of R, dnll of the bias, lse of the slice
 //                   sums, ldr the label of column 0, n_tail of the slices the number of labels (the launch has whole tiles only)
 // EPI_ADD_SUMS: a launch of slices adds its sums to those that are there ("NN": dx over the pieces of the vocabulary).
 enum { EPI_PLAIN = 0, EPI_ROWS, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD, EPI_LOSS_STATS, EPI_LOSS_GRAD, EPI_ADD_SUMS };
