@@ -64,6 +64,10 @@ class ob_lm_loss_desc(C.Structure):
     _fields_ = [("hidden", C.c_int), ("vocab", C.c_int), ("dtype", C.c_int)]
 
 
+class ob_lm_loss_launch(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("fwd_tile", "fwd_workgroups", "pieces", "piece_tile", "last_tile", "dx_tile")]
+
+
 class ob_rotary_axes_desc(C.Structure):
     _fields_ = [("head_dim", C.c_int), ("n_axes", C.c_int), ("base", C.c_float), ("per_axis", C.c_int), ("axis_of_pair", C.c_int8 * 64)]
 
@@ -138,6 +142,7 @@ _SIGNATURES = {
     "ob_varlen_attn_bwd_plan": (_I, [_SEG, _I, _I, _I, _I, C.POINTER(ob_attn_bwd_launch), _i32p, _I]),
     "ob_varlen_attn_bwd_threads": (_I, [_SEG, _I, _I, _I, _I, C.POINTER(C.c_int)]),
     "ob_lm_loss_workspace_bytes": (_Z, [C.POINTER(ob_lm_loss_desc), _I]),
+    "ob_lm_loss_plan": (_I, [C.POINTER(ob_lm_loss_desc), _I, C.POINTER(ob_lm_loss_launch)]),
     "ob_lm_loss_fwd": (_I, [C.POINTER(ob_lm_loss_desc), _P, _P, _I, _P, _P, _I, _P, _P, _P, _P, _Z, _P]),
     "ob_lm_loss_bwd": (_I, [C.POINTER(ob_lm_loss_desc), _I, _P, _P, _I, _P, _P, _I, _P, _P, _P, _P, _P, _P, _Z, _P]),
     "ob_rotary_axes": (_I, [C.POINTER(ob_rotary_axes_desc), _P, _I, _P, _I, _I, _I, _P, _I, _I, _P]),
@@ -455,6 +460,12 @@ def make_lm_loss_desc(hidden, vocab, dtype=OB_BF16) -> ob_lm_loss_desc:
 
 def ob_lm_loss_workspace_bytes(desc, n_rows) -> int:
     return lib.ob_lm_loss_workspace_bytes(C.byref(desc), n_rows)
+
+
+def ob_lm_loss_plan(desc, n_rows) -> ob_lm_loss_launch:
+    out = ob_lm_loss_launch()
+    _check(lib.ob_lm_loss_plan(C.byref(desc), n_rows, C.byref(out)))
+    return out
 
 
 def _row_list(rows, total_tokens):

@@ -1223,9 +1223,13 @@ static void nn_piece(int M, int N, int K, const void *A, int lda, const void *B,
 template <int BM, int BN>
 static void nn_round(int M, int N, float *part, void *C, hipStream_t s) {
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
-    const TailSplit ts{part, 0, tm * tn, 1, 0};
-    hipLaunchKernelGGL((tail_sum_kernel<BM, BN>), dim3(tm * tn * (BM * BN / 8 / 256)), dim3(256), 0, s, ts, M, N, tm, tn,
-                       (const __bf16 *)nullptr, (const __bf16 *)nullptr, 0, (__bf16 *)C, N, (const int32_t *)nullptr);
+    constexpr int MOST = 1 << 18;      // tiles of a launch, whose threads, one to eight values, are fewer than 2^32
+    for (int t0 = 0; t0 < tm * tn; t0 += MOST) {
+        const int n = tm * tn - t0 < MOST ? tm * tn - t0 : MOST;
+        const TailSplit ts{part + (size_t)t0 * (BM * BN), t0, n, 1, 0};
+        hipLaunchKernelGGL((tail_sum_kernel<BM, BN>), dim3(n * (BM * BN / 8 / 256)), dim3(256), 0, s, ts, M, N, tm, tn,
+                           (const __bf16 *)nullptr, (const __bf16 *)nullptr, 0, (__bf16 *)C, N, (const int32_t *)nullptr);
+    }
 }
 void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, bool first, hipStream_t s) {
     ProfScope prof(K_GEMM, s, 2.0 * M * N * K);

@@ -181,6 +181,8 @@ Plan whole_plan(int layout, int M, int N, int K) {
     double t_best = 0;
     for (TileKind kind : {BIG, SMALL, FINE}) {
         const Plan p{kind, tiles_of(kind, M, N), 0, 1, 0};
+        // (256 threads to a tile, and a launch has fewer than 2^32: short contractions would have small tiles for 2^38 results and more)
+        if (kind != BIG && p.n_full >= 1 << 24) continue;
         const double t = estimate_us(layout, kind, nk, bytes_of(M, N, K), p);
         if (kind == BIG || t < t_best) { t_best = t; best = p; }
     }

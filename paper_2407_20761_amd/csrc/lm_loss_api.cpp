@@ -99,6 +99,20 @@ extern "C" size_t ob_lm_loss_workspace_bytes(const ob_lm_loss_desc *desc, int n_
     return bytes_of(desc, n_rows);
 }
 
+extern "C" int ob_lm_loss_plan(const ob_lm_loss_desc *desc, int n_rows, ob_lm_loss_launch *launch) {
+    const char *who = "ob_lm_loss_plan";
+    if (int rc = validate_desc(desc, who)) return rc;
+    if (desc->dtype != OB_BF16) return fail(OB_EINVAL, "%s: the plan is that of bf16", who);
+    if (!launch) return fail(OB_EINVAL, "%s: launch is null", who);
+    if (!ob_lm_loss_workspace_bytes(desc, n_rows)) return fail(OB_EINVAL, "%s: n_rows %d out of range", who, n_rows);
+    const int n = n_rows, V = desc->vocab, H = desc->hidden;
+    const Pieces pc(n, V);
+    const Plan fwd = whole_plan(0, n, V, H), piece = whole_plan(0, n, pc.cols, H), last = whole_plan(0, n, V - (pc.count - 1) * pc.cols, H);
+    *launch = ob_lm_loss_launch{tile_rows(fwd.kind), fwd.n_full, pc.count, tile_rows(piece.kind), tile_rows(last.kind),
+                                pc.count > 1 ? tile_rows(whole_plan(1, n, H, pc.cols).kind) : 0};
+    return OB_OK;
+}
+
 extern "C" int ob_lm_loss_fwd(const ob_lm_loss_desc *desc, const void *w, const void *x, int total_tokens, const int32_t *rows_host,
                               const int32_t *rows_dev, int n_rows, const int32_t *labels, float *nll, float *lse, void *ws,
                               size_t ws_bytes, void *hip_stream) {
