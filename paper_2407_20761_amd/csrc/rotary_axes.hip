@@ -4,8 +4,9 @@
 // (the gradient turns back by the same angles).  A pair of axis -1 passes as it is.
 //
 // The angle: theta_i / 2 pi comes from the host as a 64-bit fraction of a turn, and position x fraction modulo 2^64 drops
-// the whole turns exactly, for every 32-bit position; the upper 32 bits, as a signed number of half turns, lose 1.5e-9 rad.
-// In floating point a position of a million keeps two digits of its angle in 32 bits.
+// the whole turns exactly, for every 32-bit position; its nearest multiple of 2^-32 of a turn is off by 7.3e-10 rad.  A float has 24 bits of that: the
+// sine and cosine of the nearest multiple of 2^-25 of a turn, which a float holds exactly, are turned on by the rest, at most 9.4e-8 rad (whose square is lost in
+// any float).  In floating point a position of a million keeps two digits of its angle in 32 bits.
 //
 // Bound by memory: each value is read and written once.  The sines and cosines of a token are the same for all its heads: a workgroup
 // works them out once per token and pair into LDS and walks the token's heads with them.
@@ -47,7 +48,11 @@ __global__ __launch_bounds__(THREADS) void rotary_axes_kernel(const E *x, int ld
         float2 v{PASSES, 0.f};
         if (axis >= 0) {
             const uint64_t turns = (uint64_t)(int64_t)pos[(size_t)axis * T + t0 + t] * table.turn[p];
-            sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &v.y, &v.x);
+            const uint32_t angle = (uint32_t)((turns + 0x80000000u) >> 32), coarse = (angle + 64u) & ~127u;      // (modulo a turn)
+            float sine, cosine;
+            sincospif((float)(int32_t)coarse * 0x1p-31f, &sine, &cosine);
+            const float rest = (float)(int32_t)(angle - coarse) * 0x1.921fb6p-30f;      // x pi / 2^31
+            v = float2{cosine - rest * sine, sine + rest * cosine};
             if (inverse) v.y = -v.y;
         }
         cs[t * half + p] = v;
