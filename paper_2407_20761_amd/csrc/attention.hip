@@ -1804,9 +1804,9 @@ __global__ __launch_bounds__(256) void attn_sink_sum_kernel(const float *__restr
 double attn_window_flops(const ob_segments *seg, int nq, int d, int window, int sinks) {
     double area = 0;
     for (int j = 0; j < seg->n_seg; ++j) {
-        const double len = seg->cu_host[j + 1] - seg->cu_host[j], w = len < window ? len : window, past = len - w, s = sinks < w ? sinks : w;
+        const double len = seg->cu_host[j + 1] - seg->cu_host[j], w = len < window ? len : window, past = len - w, s = sinks;
         area += w * (w + 1) / 2 + past * w;
-        // a row i >= w sees the sinks that have left its window: min(i + 1 - w, sinks)
+        // a row i >= w sees the sinks that have left its window, min(i + 1 - w, sinks): all of them in the end, however short the window
         area += past < s ? past * (past + 1) / 2 : s * (s + 1) / 2 + (past - s) * s;
     }
     return 4.0 * nq * d * area;
