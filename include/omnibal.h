@@ -23,7 +23,9 @@
  *   - Every call validates its arguments on the host first and returns a non-zero ob_status
  *     WITHOUT launching anything when validation fails.  ob_last_error() gives the text.
  *   - Feature dimensions (hidden, mlp_dim, head_dim * heads) must be multiples of 64; head_dim
- *     must be 64 or 128; the token count T is arbitrary (1 .. 2^22).
+ *     must be 64 or 128; the token count T is arbitrary (1 .. 2^22).  Attention in bf16 refuses
+ *     (OB_EUNSUPPORTED) what a launch has no threads for: nq times the segments' tiles of 128 rows
+ *     have to be fewer than 2^24, nkv times those of 64 rows as well (heads of 128: 2^23).
  */
 #ifndef OMNIBAL_H
 #define OMNIBAL_H

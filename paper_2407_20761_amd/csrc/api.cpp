@@ -81,6 +81,12 @@ int validate_segments(const ob_segments *seg, const char *who) {
     return OB_OK;
 }
 
+int validate_attn_launches(const ob_segments *seg, int nq, int nkv, int d, int dtype, const char *who) {
+    if (dtype == OB_BF16 && !attn_launches_fit(seg, nq, nkv, d))
+        return fail(OB_EUNSUPPORTED, "%s: %d tokens in %d segments are too many tiles of a launch for %d heads over %d", who, seg->total_tokens, seg->n_seg, nq, nkv);
+    return OB_OK;
+}
+
 }  // namespace
 
 int validate_attn(const ob_segments *seg, int nq, int nkv, int d, int ldq, int ldkv, int ldo,
@@ -92,7 +98,8 @@ int validate_attn(const ob_segments *seg, int nq, int nkv, int d, int ldq, int l
     if (mask != OB_MASK_SEG_BIDIR && mask != OB_MASK_SEG_CAUSAL) return fail(OB_EINVAL, "%s: unknown mask kind %d", who, mask);
     if (ldq < nq * d || ldo < nq * d || ldkv < nkv * d || ldq % 8 || ldkv % 8 || ldo % 8)
         return fail(OB_EINVAL, "%s: row strides must cover the heads and be multiples of 8 elements", who);
-    return validate_segments(seg, who);
+    if (int rc = validate_segments(seg, who)) return rc;
+    return validate_attn_launches(seg, nq, nkv, d, dtype, who);
 }
 
 namespace {
@@ -306,6 +313,7 @@ static int validate_block(const ob_block_desc *desc, const ob_block_weights *w, 
         if (desc->norm == OB_LAYERNORM && (!w->n1_b || !w->n2_b)) return fail(OB_EINVAL, "%s: has_bias set but a beta pointer is null", who);
     }
     if (int rc = validate_segments(seg, who)) return rc;
+    if (int rc = validate_attn_launches(seg, desc->n_q_heads, desc->n_kv_heads, desc->head_dim, desc->dtype, who)) return rc;
     if (!saved || saved_bytes < ob_block_saved_bytes(desc, seg->total_tokens))
         return fail(OB_EWORKSPACE, "%s: saved buffer too small (%zu bytes given)", who, saved_bytes);
     if (!ws || ws_bytes < ob_block_workspace_bytes(desc, seg->total_tokens))

@@ -43,7 +43,6 @@ constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 constexpr float NEG_BIG = -1.0e30f;
 constexpr float RESCALE_LOG2 = 8.0f;  // the forward's reference maximum may lag the row maximum by this much (base-2 log)
-constexpr int QT = 128;  // rows owned by a workgroup (4 waves x 32)
 constexpr int WAIT_VM0 = 0x0F70;  // s_waitcnt vmcnt(0) only
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -56,6 +56,13 @@ int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side,
     return n << log2;
 }
 
+bool attn_launches_fit(const ob_segments *seg, int nq, int nkv, int d) {
+    const long most = 1l << 24, most_kv = d == 128 ? 1l << 23 : 1l << 24;
+    // (tiles are no more than this: the usual batch is not counted)
+    if (((long)seg->total_tokens / QT + seg->n_seg) * nq < most && ((long)seg->total_tokens / 64 + seg->n_seg) * nkv < most_kv) return true;
+    return (long)count_tiles(seg, QT) * nq < most && (long)count_tiles(seg, 64) * nkv < most_kv;
+}
+
 int sink_chunks(const ob_segments *seg, int whole, int sinks, int *segments) {
     int n = 0, split = 0;
     for (int j = 0; j < seg->n_seg && sinks; ++j) {

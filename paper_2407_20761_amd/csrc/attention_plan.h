@@ -9,6 +9,7 @@
 namespace ob {
 
 constexpr int ST = 64;   // rows of a streamed tile
+constexpr int QT = 128;  // rows owned by a workgroup of the forward and dQ (4 waves x 32)
 
 // Order of the tiles: heaviest first.  The work of a tile is the number of streamed tiles it walks;
 // in a causal batch that differs by an order of magnitude between the first and the last tile of a
@@ -51,6 +52,10 @@ __host__ __device__ constexpr uint32_t dkv_piece_offset(uint32_t voff, uint32_t 
 // (window > 0: causal, a row sees no more than that many keys; the first tile of key rows of a segment of up to `whole` is seen by all its rows)
 int make_order(const ob_segments *seg, int tile_rows, bool causal, bool kv_side, TileOrder &ord, int window = 0, int whole = 0);
 int dkv_shape(const ob_segments *seg, int nkv, int group, int d, bool causal, int window = 0, int whole = 0);
+
+// A launch has fewer than 2^32 threads (of one with more the runtime runs a part and reports nothing): 256 to a tile of 128 query rows and head, and of dK / dV
+// up to 256 (heads of 128: 512, in blocks) to a tile of 64 key rows and head.
+bool attn_launches_fit(const ob_segments *seg, int nq, int nkv, int d);
 
 constexpr int MAX_SINKS = 64;      // they lie in a segment's first tile of keys
 // The sinks of a segment are seen by all of its rows.  Up to sink_whole_rows() the workgroup of its first keys walks them all: what that adds to its
