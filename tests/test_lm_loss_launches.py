@@ -14,6 +14,54 @@ def _plan(n, H, V):
     return ob.ob_lm_loss_plan(ob.make_lm_loss_desc(H, V), n)
 
 
+# ---- every kind of tile ------------------------------------------------------------------------------
+
+# (rows, all tokens, hidden, vocabulary) -> tiles of the forward's logits, pieces, tiles of the logits of a piece, of the last, of dx's sums
+LAUNCHES = [
+    ((2100, 2100, 1024, 16384), (256, 1, 256, 256, 0)),           # whole columns of tiles, ragged rows
+    ((2060, 5000, 1024, 16385), (256, 1, 256, 256, 0)),           # ragged both ways, listed rows
+    ((2049, 2049, 4096, 8200), (256, 1, 256, 256, 0)),
+    ((2100, 2100, 256, 16384), (128, 1, 128, 128, 0)),
+    ((257, 300, 768, 2001), (64, 1, 64, 64, 0)),
+    ((4100, 4100, 64, 131080), (128, 2, 128, 128, 64)),
+    ((4100, 4200, 1024, 131080), (256, 2, 256, 256, 128)),
+    ((4100, 4100, 2048, 131080), (256, 2, 256, 256, 256)),
+    ((9000, 9000, 1024, 120001), (256, 3, 256, 256, 256)),        # the sums of three pieces
+]
+
+
+@pytest.mark.parametrize("sizes,want", LAUNCHES)
+def test_which_launches_a_case_takes(sizes, want):
+    n, _, H, V = sizes
+    p = _plan(n, H, V)
+    assert (p.fwd_tile, p.pieces, p.piece_tile, p.last_tile, p.dx_tile) == want
+
+
+@gpu
+@pytest.mark.parametrize("sizes", [s for s, _ in LAUNCHES])
+def test_every_launch(sizes):
+    n, T, H, V = sizes
+    c = Call(T, H, V, rows=None if n == T else _some_rows(T, n), seed=n).run()
+    c.check()
+    first = c.dx.clone(), c.dw.clone()
+    for t in (c.dx, c.dw):
+        t.fill_(float("nan"))
+    c.bwd()
+    assert torch.equal(first[0], c.dx) and torch.equal(first[1], c.dw)
+
+
+@gpu
+def test_accumulation_over_pieces_in_the_largest_tiles():
+    c = Call(4100, 2048, 131080, seed=3)
+    old = torch.randn(c.dw.shape, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).bfloat16() * 0.1
+    c.fwd()
+    c.dw.copy_(old)
+    c.bwd(ob.OB_BWD_ACCUMULATE)
+    value, bound = expected(c.w, c.x, c.labels, c.dnll, U)["dw"]
+    value = value + old.double()
+    assert float(((c.dw.double() - value).abs() / (bound + U * value.abs())).max()) <= 1
+
+
 # ---- limits ----------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("H", [64, 128, 256, 320, 4096])
