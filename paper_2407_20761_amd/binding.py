@@ -190,9 +190,12 @@ def _ptr(t):
 
 
 def _ptr_i32(t):
-    """of a tensor of 32-bit whole numbers (labels, positions: torch makes them with 64 unless told otherwise)"""
+    """of a tensor of 32-bit whole numbers, one behind the other (labels, positions: torch makes them with 64 unless told otherwise, and positions
+    kept token by token are a view with strides once they are transposed)"""
     if t is not None and t.dtype != torch.int32:
         raise TypeError(f"expected int32, got {t.dtype}")
+    if t is not None and not t.is_contiguous():
+        raise ValueError(f"expected a contiguous tensor, got strides {t.stride()} of shape {tuple(t.shape)}")
     return _ptr(t)
 
 
