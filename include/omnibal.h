@@ -137,10 +137,13 @@ int ob_varlen_attn_bwd_static(const void *d_o, const void *q, const void *k, con
 /* ---- varlen attention with a sliding window and sinks ------------------------------------------
  * As above, causal, with allowed(i, j) <=> same segment, j <= i, and (i - j < window or j is one of the segment's first
  * `sinks` tokens).  window >= 1 (a row sees itself: none is empty; a window as long as the segments is plain causal
- * attention), 0 <= sinks <= 64, 1e-20 <= scale <= 1e6, scores up to 2^20 in magnitude (beyond, fp32 sums do not tell
- * probabilities); row strides up to 2^24 elements, tensors and workspace aligned to 16 bytes.  Key
+ * attention), 0 <= sinks <= 64, 1e-20 <= scale <= 1e6, scores up to 2^20 in magnitude (lse is good to 2e-7 of its value: at
+ * 2^20 a probability of the backward is known to 22 %); row strides up to 2^24 elements, tensors and workspace aligned to 16 bytes.  Key
  * tiles that no row of a workgroup sees are not computed, so a call costs tokens * window, not tokens^2.  Nothing of another segment is
  * read on a segment's behalf; inside a segment an infinity or NaN in a row of k, v or d_o may also reach rows near it that do not see it.
+ * In bf16 the operands of the matrix products are bf16, P in front of V and dO, dS in front of K and Q, and Delta beyond windows of 193 comes from o:
+ * with N(0, 1) values o is 0.0020 off in norm, the gradients 0.0024 (0.0017 of it the rounding of the results).  Keys that share a component three times
+ * their deviation: dQ 0.0057, 0.007 - 0.008 beyond windows of 193.
  * The backward's workspace (ob_varlen_attn_window_bwd_workspace_bytes for the same arguments; 0 if they are refused) holds the
  * row statistics and, for the sinks of segments much longer than the window, the fp32 sums over chunks of their queries, which are
  * added in order: no atomics, results are bitwise reproducible. */
@@ -278,14 +281,16 @@ int ob_connector_bwd(const ob_connector_desc *desc, const ob_connector_weights *
  *   G_rv = (exp(z_rv - lse_r) - [v = label_r]) dnll_r,   dx_r = sum_v G_rv W_v,   dW_v = sum_r G_rv x_r
  * The logits are never stored: the forward reduces each tile of them where it is computed, the backward computes them again
  * a piece of the vocabulary at a time (at most 1 GiB of G in bf16, or 256 columns; dx is summed over the pieces in fp32, in order).  No
- * atomics: results are bitwise reproducible.
+ * atomics: results are bitwise reproducible.  In bf16 G is rounded once, the operand of both products: dx and dw 0.0024 off in norm (0.0017 the rounding
+ * of the results), up to 0.004 of a few rows, whose entry at the label is most of G.
  * x [total_tokens, hidden], w [vocab, hidden].  rows (int32, n_rows entries, host and device copies): the supervised rows,
  * ascending, checked on the host; both NULL: every row (n_rows = total_tokens).  n_rows = 0 is a batch without a supervised
  * row: nothing is read but the sizes, dx and (without OB_BWD_ACCUMULATE) dw are zeros.  Visual tokens and prompts have no label, so a
  * packed batch has far fewer rows here than tokens.  labels, nll, lse, dnll: device memory, n_rows entries.  A row whose label is
  * outside [0, vocab) is ignored: nll 0, no gradient whatever its dnll (x of a listed row has to be finite).
  * ob_lm_loss_bwd, given lse of the forward, writes every row of dx (rows not listed: zeros) and dw (flags: OB_BWD_ACCUMULATE
- * adds to dw).  ws (ob_lm_loss_workspace_bytes) need not be kept between the two.  dtype OB_BF16, or OB_FP32 for the debug variant (x,
+ * adds to dw).  ws (ob_lm_loss_workspace_bytes, which does not always grow with n_rows: a buffer for several has the most of theirs) need
+ * not be kept between the two.  dtype OB_BF16, or OB_FP32 for the debug variant (x,
  * w, dx, dw fp32; plain kernels); hidden a multiple of 64 up to 8192, vocab up to 2^21, n_rows * vocab up to 2^39,
  * tensors and ws aligned to 16 bytes. */
 typedef struct {
@@ -317,7 +322,7 @@ int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void *w, const 
  * x: rows of n_heads heads of head_dim elements at row stride ldx, y at ldy (in elements, multiples of 8; both pointers
  * aligned to 16 bytes), so the query and key heads of a [T, (nq + 2 nkv) d] buffer are one call; y may be x (then ldy =
  * ldx), otherwise they may not overlap.  Only the columns of the heads are written.  pos: device memory, [n_axes][total_tokens],
- * any 32-bit values.  The angle is exact to 2e-9 rad at every position.  dtype OB_BF16 or OB_FP32. */
+ * any 32-bit values.  The angle is exact to 2e-9 rad at every position (bases below 10: 3e-9).  dtype OB_BF16 or OB_FP32. */
 #define OB_ROTARY_MAX_AXES 8
 #define OB_ROTARY_MAX_HEADS 4096
 typedef struct {
@@ -332,7 +337,7 @@ int ob_rotary_axes(const ob_rotary_axes_desc *desc, const void *x, int ldx, void
 /* ---- a block with these in its attention ----------------------------------------------------------
  * The block of `desc` with a window (0: none; else the mask has to be causal) and sinks as in ob_varlen_attn_window_fwd, and
  * with `rotary` (NULL: as desc says) rotary positions of several axes on its query and key heads (desc->use_rotary 0; pos:
- * device memory, [n_axes][total_tokens]).  Everything else as ob_block_fwd / ob_block_bwd, `saved` (ob_block_saved_bytes) and
+ * device memory, [n_axes][total_tokens]).  The backward turns the rounded dQ and dK in a pass of its own, which rounds them again.  Everything else as ob_block_fwd / ob_block_bwd, `saved` (ob_block_saved_bytes) and
  * ob_block_saved_offset among it; the workspace of the backward is ob_block_attn_workspace_bytes (0: refused arguments), of
  * the forward ob_block_workspace_bytes will do. */
 typedef struct {

@@ -675,10 +675,17 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 2) void attn_fwd_kernel(
 // on one half of the tile with their partial dQ added at the end, asked the L2 for twice the bytes
 // per MFMA (4.7 GB per launch on the 7B-shaped batch, 10 TB/s) and had a barrier per 24 MFMAs.
 // ------------------------------------------------------------------------------------------------
-// Delta of a windowed row that sees few keys.  From the o of 8 bits it is off by as much as dS's own rounding (two keys to a row: dQ and dK 0.0046 off, 0.0024
-// without).  sum_j P_j (dP_j - Delta) over the row is 0 but for that, so it is what Delta lacks: workgroups of a short walk find it in a pass of its own (DELTA)
-// before they begin, and dK / dV, behind this kernel, takes it from them.  Added up in every walk's own pass it would serve dK alone, for an
-// addition to each score: dQ of a window of 1024 4 % slower in heads of 128, 8 % in heads of 64, gradients of 0.0024 - 0.0025 to 0.0024.
+// Delta of a windowed row.  From the o of 8 bits it is off, and sum_j P_j (dP_j - Delta) over the row is 0 but for that, so it is what Delta lacks:
+// workgroups of a short walk find it in a pass of its own (DELTA) before they begin, and dK / dV, behind this kernel, takes it from them.  What it buys and costs
+// (heads of 128, a segment of 16384, 32 / 8 heads; error of dQ in norm without and with it, its own two roundings 0.0023; N(0, 1) values, keys then with a component
+// shared by all of them of 1 and of 3 times their deviation, which Delta's error multiplies in dQ):
+//   window          2              8              64             128            193            256            1024
+//   shared 0    0.0037 0.0024  0.0027 0.0024  0.0024 0.0023  0.0024 0.0024  0.0024 0.0024  0.0024 0.0023  0.0025 0.0024
+//   shared 1    0.0053 0.0023  0.0040 0.0029  0.0036 0.0028  0.0038 0.0029  0.0039 0.0029  0.0040 0.0029  0.0038 0.0029
+//   shared 3    0.0122 0.0023  0.0093 0.0054  0.0084 0.0053  0.0093 0.0057  0.0093 0.0057  0.0094 0.0057  0.0094 0.0056
+//   dQ, us        170 205        169 204        174 211        189 242        204 266        210 304        417 723
+// Without a shared component it falls as 1 / sqrt(keys) and shows up to 8 keys or so; with one it is the same at every length, and the limit is what it may cost: a third
+// of dQ, not two.  Added up in every walk's own pass it would serve dK alone, for an addition to each score (dQ of a window of 1024 4 % slower in heads of 128, 8 % in heads of 64).
 constexpr int SHORT_WALK = 5;      // tiles of the band: windows up to 193, the first 256 rows of every segment
 template <int D, bool CAUSAL, bool MASK, bool BAND = false, bool DELTA = false>
 __device__ __forceinline__ void dq_half(const unsigned char OB_LDS *__restrict__ ks,

@@ -84,6 +84,10 @@ int sink_chunks(const ob_segments *seg, int whole, int sinks, int *segments) {
 // not hold their lengths) the picks are 0.25 % slower in the mean than the fastest shape; fifteen more than 3 %, the worst 7.6 % (one segment of 7168, 10
 // heads of 64: 166 us, with tiles of 64 154).  Eight of the fifteen are one bias: bidirectional launches of heads of 128 that keep four pairs where blocks are
 // 3.3 - 5.5 % faster (five ViT tiles, 48 / 8 heads: 328 us, blocks 311).
+// With a window the same constants, a tile's walk cut off behind it.  Over 372 launches (profiles/window_dkv_shape_choice.csv: windows of 64 - 4096, one segment, packed
+// samples and texts of 129 - 32768 tokens, 1 - 16 key / value heads, groups of 1 - 6, no sinks) the picks are 0.5 % slower in the mean than the faster shape; fourteen
+// more than 3 %, the worst 22: launches of heads of 128 that fill the chip about once (4096 tokens in samples, 48 / 8 heads, window 1024: 180 us in four pairs, blocks 152;
+// one head over 16384 tokens, window 64, the other way: 19.9 and 16.3) and one long segment in heads of 64 (32768 tokens, 6 / 1 heads, window 1024: 159 and 144).
 namespace {
 struct DkvShape { int kv_rows; double full, chain, ends; };
 constexpr DkvShape DKV_64[] = {{64, 0.81, 1.1, 0}, {64, 0.70, 1.53, 0}};                                // SR = 64, SR = 32 (six pairs: below)

@@ -59,9 +59,14 @@ bool attn_launches_fit(const ob_segments *seg, int nq, int nkv, int d);
 
 constexpr int MAX_SINKS = 64;      // they lie in a segment's first tile of keys
 // The sinks of a segment are seen by all of its rows.  Up to sink_whole_rows() the workgroup of its first keys walks them all: what that adds to its
-// walk, rows past the window times the heads of a group, is to cost less than the two launches of the other way (about 25 trips of 64 rows).
-// Beyond, chunks of its rows leave fp32 sums, of 128 rows while that is few chunks (one segment of 557, 32 / 8 heads of 128, window 128: dK / dV 54 -> 45 us
-// against 256; one of 65521, 64 sinks, window 512 420 -> 437).  All of this is the segment's own, so that it gives the same sums in every batch.
+// walk, rows past the window times the heads of a group, is to cost less than the two launches of the other way (about 25 trips of 64 rows).  Measured, 4 sinks, windows of
+// 128 and 1024, dK / dV whole and in chunks: at 1600 rows times heads one segment alone takes 36 and 20 us (group 1, heads of 64), 57 and 47 (group 4, heads of 128);
+// at 800 29 and 24, at 400 chunks are the slower way; six segments that fill the chip (8 key / value heads of 128, group 4, window 1024) 305 and 345 at
+// 3200, 492 and 521 at 6400.  So the limit stands between the two, as it has to be the segment's own: up to 1.8 times slower than chunks for one segment of
+// group 1 just below it, 13 % slower than whole for a full chip above it.
+// Beyond, chunks of its rows leave fp32 sums, of 128 rows up to 4096, of 256 from there (dK / dV, windows of 128 and 512: one segment of 4096, 128 rows are 1 - 24 % faster;
+// of 8192 from 4 % slower, 16 heads, to 20 % faster, 8 / 2 heads; of 16384 from 8 % slower to 16 % faster; of 65521 4 % slower to 3 % faster).
+// All of this is the segment's own, so that it gives the same sums in every batch.
 constexpr int SINK_SR = 32;      // query rows of a streamed tile
 __host__ __device__ constexpr int sink_chunk_rows(int len) { return len <= 4096 ? 128 : 256; }
 __host__ __device__ constexpr int sink_chunks_of(int len) { return (len + sink_chunk_rows(len) - 1) / sink_chunk_rows(len); }

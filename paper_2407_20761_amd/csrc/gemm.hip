@@ -528,8 +528,8 @@ struct KLoop {
 //   EPI_GELU        C = x (+ bias), act[m, n] = GELU(C), act in place of R
 //   EPI_GELU_BWD    C = x GELU'(up), up in place of R
 //   EPI_SWIGLU_BWD  C[m, n], C[m, N + n]: the gradients of gate and up for x, that of their product; up [M, 2 N] in place of R
-// The last two leave the fp32 sums of each half tile's columns of C at colsum[2 tile_m + wave row][C's columns] (may be null: in place of the bias).
-// The last two are those of the cross entropy over a vocabulary, whose logits z = x W^T ("NT") are not stored:
+// EPI_GELU_BWD and EPI_SWIGLU_BWD leave the fp32 sums of each half tile's columns of C at colsum[2 tile_m + wave row][C's columns] (may be null: in place of the bias).
+// EPI_LOSS_STATS and EPI_LOSS_GRAD are those of the cross entropy over a vocabulary, whose logits z = x W^T ("NT") are not stored:
 //   EPI_LOSS_STATS  per row of z and column half of a tile its maximum and the sum of exp(z - maximum): float2 [2 tiles_n][M] in place of C; the logit of
 //                   the row's label (in place of R) to float [M] in place of the bias, by the lane that holds it
 //   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) dnll, zeros in the columns N .. ldc, rounded once, to bf16: the operand of two products; labels in place of R, dnll of the bias, lse of the slice
@@ -1175,7 +1175,7 @@ int gemm_any(int layout, int M, int N, int K, const void *A, const void *B, void
 }
 
 // ---- cross entropy over a vocabulary ----------------------------------------------------------------
-// z = A B^T, [M, N] over K, in whole tiles of p (loss_plan), in pieces of the columns where the caller cuts B
+// z = A B^T, [M, N] over K, in whole tiles of p (whole_plan()), in pieces of the columns where the caller cuts B
 template <int EPI>
 static void launch_loss(const Plan &p, int M, int N, int K, const void *A, const void *B, void *C, int ldc, const void *bias, const void *side,
                         int ldr, const TailSplit &ts, hipStream_t s) {

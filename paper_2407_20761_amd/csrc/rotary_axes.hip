@@ -37,7 +37,10 @@ __device__ __forceinline__ void turn(const V a, const V b, const float2 *cs, V &
 }
 
 // V: 16 bytes of N elements E.  x and y may be the same tensor: a thread reads what it writes, and nothing else.  STREAM: results that do not fit the L2s beside x are
-// stored past them (16327 tokens, 40 heads of 128: 335 MB in 51.5 us, 6.5 TB/s, 66 through them; a large copy runs at 5.4), smaller ones stay for their reader.
+// stored past them, smaller ones stay for their reader.  Tensors that no call has touched before, 40 heads of 128, through the L2s and past them: 16327 tokens (334 MB)
+// 66.6 and 63.3 us (5.3 TB/s; the same tensors again and again 63.3 and 51.0), 4096 18.5 and 18.0, 2048 11.5 and 10.9, 1024 (below the limit) 9.0 and 8.6.  With the
+// windowed attention behind it in a block, the two together: 16327 tokens 380.3 and 379.5 us, 4096 100.4 and 99.5, 2048 52.6 and 53.8.  An elementwise pass that reads the
+// results at once loses up to 8 % (16327 tokens, both launches: 121 and 131).
 template <class V, class E, int N, bool STREAM>
 __global__ __launch_bounds__(THREADS) void rotary_axes_kernel(const E *x, int ldx, E *y, int ldy, int T, int n_heads, int half,
                                                               RotaryTable table, const int32_t *__restrict__ pos, int inverse) {

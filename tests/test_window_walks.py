@@ -174,6 +174,18 @@ def _spread(c, window, sinks):
     return 0.24 * out + 1e-6
 
 
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [1e-20, 1e6])
+def test_scales_at_their_limits(scale, d):
+    """the smallest makes every score 0, against which a masked one has to be far below; at the largest a masked one has to be finite"""
+    c = _call([300, 5, 64], 2, 1, d, 40, 4)
+    if scale > 1:
+        _split(c.qkv, 2, 1, d)[0].mul_(1e-6 * d ** -0.5)
+    c.scale = scale
+    c.run().check()
+
+
 # ---- the profile ---------------------------------------------------------------------------------------
 
 
