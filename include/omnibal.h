@@ -281,8 +281,8 @@ int ob_connector_bwd(const ob_connector_desc *desc, const ob_connector_weights *
  *   G_rv = (exp(z_rv - lse_r) - [v = label_r]) dnll_r,   dx_r = sum_v G_rv W_v,   dW_v = sum_r G_rv x_r
  * The logits are never stored: the forward reduces each tile of them where it is computed, the backward computes them again
  * a piece of the vocabulary at a time (at most 1 GiB of G in bf16, or 256 columns; dx is summed over the pieces in fp32, in order).  No
- * atomics: results are bitwise reproducible.  In bf16 G is rounded once, the operand of both products: dx and dw 0.0024 off in norm (0.0017 the rounding
- * of the results), up to 0.004 of a few rows, whose entry at the label is most of G.
+ * atomics: results are bitwise reproducible.  In bf16 G is rounded, the operand of both products, and what that takes of the entries at the labels, most of a
+ * row of dx and of a label's row of dw, is added to the products in fp32: dx and dw are off by their own rounding (0.0017 in norm) and next to nothing else.
  * x [total_tokens, hidden], w [vocab, hidden].  rows (int32, n_rows entries, host and device copies): the supervised rows,
  * ascending, checked on the host; both NULL: every row (n_rows = total_tokens).  n_rows = 0 is a batch without a supervised
  * row: nothing is read but the sizes, dx and (without OB_BWD_ACCUMULATE) dw are zeros.  Visual tokens and prompts have no label, so a

@@ -532,10 +532,12 @@ struct KLoop {
 // EPI_LOSS_STATS and EPI_LOSS_GRAD are those of the cross entropy over a vocabulary, whose logits z = x W^T ("NT") are not stored:
 //   EPI_LOSS_STATS  per row of z and column half of a tile its maximum and the sum of exp(z - maximum): float2 [2 tiles_n][M] in place of C; the logit of
 //                   the row's label (in place of R) to float [M] in place of the bias, by the lane that holds it
-//   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) dnll, zeros in the columns N .. ldc, rounded once, to bf16: the operand of two products; labels in place of R, dnll of the bias, lse of the slice
-//                   sums, ldr the label of column 0, n_tail of the slices the number of labels (the launch has whole tiles only)
+//   EPI_LOSS_GRAD   C = (exp(z - lse) - [column is the label]) dnll, zeros in the columns N .. ldc, rounded to bf16: the operand of two products; labels in place of R, dnll of the bias, lse of the slice
+//                   sums, ldr the label of column 0, n_tail of the slices the number of labels (the launch has whole tiles only).  Behind C: float [M], what a row's entry at
+//                   its label lost in the rounding, by the lane that has it; int32 [ldc], -1 (loss_lack(), loss_lead())
+//   EPI_LOSS_DW     ("TN") C = x (+ R); rows of C with an entry r >= 0 in that list behind A get row r of the bias' [K, N] added before they are rounded
 // EPI_ADD_SUMS: a launch of slices adds its sums to those that are there ("NN": dx over the pieces of the vocabulary).
-enum { EPI_PLAIN = 0, EPI_ROWS, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD, EPI_LOSS_STATS, EPI_LOSS_GRAD, EPI_ADD_SUMS };
+enum { EPI_PLAIN = 0, EPI_ROWS, EPI_LOSS_DW, EPI_GELU, EPI_GELU_BWD, EPI_SWIGLU_BWD, EPI_LOSS_STATS, EPI_LOSS_GRAD, EPI_ADD_SUMS };
 constexpr float LOG2E = 1.4426950408889634f;
 
 // EPI_LOSS_STATS, straight from the accumulators: a lane holds, of rows 16 i + lane % 16, columns 16 j + 4 (lane / 16) .. + 3 of the wave's part, so a
@@ -674,7 +676,7 @@ __device__ __forceinline__ void gemm_tile(
     float bv[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) bv[e] = 0.f;
-    if (EPI < EPI_GELU_BWD && bias && n_out < N) {
+    if (EPI < EPI_GELU_BWD && EPI != EPI_LOSS_DW && bias && n_out < N) {
         const bf16x8 b8 = *(const bf16x8 *)(bias + n_out);
 #pragma unroll
         for (int e = 0; e < 8; ++e) bv[e] = (float)b8[e];
@@ -689,6 +691,9 @@ __device__ __forceinline__ void gemm_tile(
     if constexpr (EPI == EPI_LOSS_GRAD) {
         const int32_t *labels = (const int32_t *)side;
         const float *lse = ts.part, *dnll = (const float *)bias;
+        float *const lack = loss_lack(Cm, M, ldc);
+        if (tile_m == 0)
+            for (int i = n0 + tid; i < min(n0 + BN, ldc); i += C::NW * 64) loss_lead(Cm, M, ldc)[i] = -1;
         put(0);
 #pragma unroll
         for (int ii = 0; ii < TA / 2; ++ii) {
@@ -717,6 +722,13 @@ __device__ __forceinline__ void gemm_tile(
                     const float p = __builtin_amdgcn_exp2f(z * LOG2E - lse2[r]) - (e == rel ? 1.f : 0.f);
                     g[e] = (__bf16)(weight[r] == 0.f || n_out + e >= N ? 0.f : p * weight[r]);
                 }
+                if (rel >= 0 && rel < 8 && n_out + rel < N && m < M) {      // (few lanes of few waves: the entry once more)
+                    float z = lo[r][0];
+#pragma unroll
+                    for (int e = 1; e < 8; ++e) z = e == rel ? e < 4 ? lo[r][e & 3] : hi[r][e & 3] : z;
+                    const float exact = weight[r] == 0.f ? 0.f : (__builtin_amdgcn_exp2f(z * LOG2E - lse2[r]) - 1.f) * weight[r];
+                    lack[m] = exact - (float)(__bf16)exact;
+                }
                 if (m < M && n_out < ldc) *(bf16x8 *)(Cm + (size_t)m * ldc + n_out) = g;      // (the next products read it: through the caches)
             }
         }
@@ -739,6 +751,11 @@ __device__ __forceinline__ void gemm_tile(
         // take those (16400 x 3200 x 3200, NT: 285 us with the loads pair by pair, 265, 252 without a residual; weight gradient
         // 9600 x 3200 over 3075 rows, accumulated: 166, 151, 145).  Registers of the K loop's fragments hold them.
         bf16x8 res[MODE == 1 ? TA / 2 : 1][NR];
+        int OB_LDS *const lead = (int OB_LDS *)(slab + 32 * RSTR);      // (EPI_LOSS_DW) of the wave's rows
+        if constexpr (EPI == EPI_LOSS_DW) {
+            static_assert(32 * RSTR + BM / WM * 4 <= 4 * C::SLOT / C::NW, "behind the slab");
+            for (int i = lane; i < BM / WM; i += 64) lead[i] = loss_lead(A, K, lda)[min(m0 + wm * (BM / WM) + i, M - 1)];
+        }
         if constexpr (MODE == 1) {
 #pragma unroll
             for (int ii = 0; ii < TA / 2; ++ii)
@@ -761,6 +778,14 @@ __device__ __forceinline__ void gemm_tile(
             if (ii + 1 < TA / 2) put(ii + 1);
             const int m_first = m0 + wm * (BM / WM) + ii * 32 + lane / LPR;
             bf16x8 r8[NR], g8[NR];
+            if constexpr (EPI == EPI_LOSS_DW) {
+#pragma unroll
+                for (int r = 0; r < NR; ++r) {
+                    const int row = lead[ii * 32 + r * RPI + lane / LPR];
+                    r8[r] = bf16x8{};
+                    if (row >= 0 && n_out < N) r8[r] = *(const bf16x8 *)(bias + (size_t)row * N + n_out);
+                }
+            }
             if constexpr (EPI == EPI_GELU_BWD || EPI == EPI_SWIGLU_BWD) {
 #pragma unroll
                 for (int r = 0; r < NR; ++r)
@@ -788,6 +813,10 @@ __device__ __forceinline__ void gemm_tile(
                     if (MODE == 1) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) o8[e] += (float)res[ii][r][e];
+                    }
+                    if constexpr (EPI == EPI_LOSS_DW) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) o8[e] += (float)r8[r][e];
                     }
                     bf16x8 o;
 #pragma unroll
@@ -857,7 +886,7 @@ __device__ __forceinline__ void gemm_tile(
     else out(integral_constant<int, 0>{}, integral_constant<bool, true>{});
 }
 
-// EPI other than plain: R is the row list, act or up (one more argument would make the argument block 128 bytes long, and a launch of that is 0.2 us
+// EPI other than plain and EPI_LOSS_DW: R is the row list, act or up (one more argument would make the argument block 128 bytes long, and a launch of that is 0.2 us
 // slower: 2567 x 768 x 256 6.0 -> 6.2)
 template <int BM, int BN, int WM, int WN, bool AK, bool BKM, int NS, int EPI = EPI_PLAIN>
 __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(
@@ -872,7 +901,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_kernel(
     const int tail_tile = sliced ? xcd_chunk((pid - n_whole) % ts.n_tail, ts.n_tail, interleave) : 0;
     int tile_m, tile_n;
     tile_of_id(sliced ? n_whole + tail_tile : xcd_chunk(pid, n_whole, interleave), tiles_m, tiles_n, tile_m, tile_n);
-    gemm_tile<BM, BN, WM, WN, AK, BKM, NS, EPI>(M, N, K, A, lda, B, ldb, Cm, ldc, bias, EPI == EPI_PLAIN ? R : nullptr, ldr, tile_m, tile_n,
+    gemm_tile<BM, BN, WM, WN, AK, BKM, NS, EPI>(M, N, K, A, lda, B, ldb, Cm, ldc, bias, EPI == EPI_PLAIN || EPI == EPI_LOSS_DW ? R : nullptr, ldr, tile_m, tile_n,
                                                 sliced, kz, tail_tile, ts, R);
 }
 
@@ -947,6 +976,9 @@ OB_GEMM_INSTANCE(64, 64, false, false, 8, EPI_LOSS_STATS)
 OB_GEMM_INSTANCE(256, 256, false, false, 4, EPI_LOSS_GRAD)
 OB_GEMM_INSTANCE(128, 128, false, false, 4, EPI_LOSS_GRAD)
 OB_GEMM_INSTANCE(64, 64, false, false, 8, EPI_LOSS_GRAD)
+OB_GEMM_INSTANCE(256, 256, true, true, 4, EPI_LOSS_DW)
+OB_GEMM_INSTANCE(128, 128, true, true, 4, EPI_LOSS_DW)
+OB_GEMM_INSTANCE(64, 64, true, true, 8, EPI_LOSS_DW)
 OB_GEMM_INSTANCE(256, 256, false, true, 4, EPI_ADD_SUMS)
 OB_GEMM_INSTANCE(128, 128, false, true, 4, EPI_ADD_SUMS)
 OB_GEMM_INSTANCE(64, 64, false, true, 8, EPI_ADD_SUMS)
@@ -1197,15 +1229,25 @@ void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, cons
     launch_loss<EPI_LOSS_GRAD>(p, n, cols, H, x, w, g, ldg, dnll, labels, first, TailSplit{(float *)lse /* read only */, p.n_full, V, 1, 0}, s);
 }
 
-// "NN" and "TN" with operands whose rows are longer than the product's; ws: as for gemm_any()
-void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *B, void *C, void *ws, size_t ws_bytes, hipStream_t s) {
+// "NN" with an A whose rows are longer than the product's; ws: as for gemm_any()
+void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *R, void *ws, size_t ws_bytes, hipStream_t s) {
     ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
     float *part = ws && ws_bytes >= gemm_workspace_bytes(1, M, N, K) ? (float *)ws : nullptr;
-    launch_layout<false, true>(1, M, N, K, A, lda, B, N, C, N, nullptr, nullptr, 0, part, s);
+    launch_layout<false, true>(1, M, N, K, A, lda, B, N, C, N, nullptr, R, N, part, s);
 }
-void launch_gemm_tn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *R, hipStream_t s) {
+// dW of a piece: "TN" in whole tiles; own [K, N]: what the columns' rows lack
+template <int BM, int NS>
+static void loss_dw(int M, int N, int K, const void *G, int ldg, const void *x, void *dw, const void *R, const void *own, hipStream_t s) {
+    const int tm = (M + BM - 1) / BM, tn = (N + BM - 1) / BM;
+    hipLaunchKernelGGL((gemm_kernel<BM, BM, 2, 2, true, true, NS, EPI_LOSS_DW>), dim3(tm * tn), dim3(256), 0, s, M, N, K, (const __bf16 *)G, ldg,
+                       (const __bf16 *)x, N, (__bf16 *)dw, N, (const __bf16 *)own, (const __bf16 *)R, N, tm, tn, TailSplit{nullptr, 0, 0, 1, 0});
+}
+void launch_loss_dw(int M, int N, int K, const void *G, int ldg, const void *x, void *dw, const void *R, const void *own, hipStream_t s) {
     ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
-    launch_layout<true, true>(2, M, N, K, A, lda, B, N, C, N, nullptr, R, N, nullptr, s);
+    const TileKind kind = make_row_cut(2, M, N, K, 0).rest.kind;
+    if (kind == BIG) loss_dw<256, 4>(M, N, K, G, ldg, x, dw, R, own, s);
+    else if (kind == SMALL) loss_dw<128, 4>(M, N, K, G, ldg, x, dw, R, own, s);
+    else loss_dw<64, 8>(M, N, K, G, ldg, x, dw, R, own, s);
 }
 
 // An "NN" product whose contraction comes in pieces that are not in memory at one time: the first leaves fp32 sums of all its tiles, like the slices of a
@@ -1221,14 +1263,14 @@ static void nn_piece(int M, int N, int K, const void *A, int lda, const void *B,
 #undef OB_ARGS
 }
 template <int BM, int BN>
-static void nn_round(int M, int N, float *part, void *C, hipStream_t s) {
+static void nn_round(int M, int N, float *part, void *C, const void *R, hipStream_t s) {
     const int tm = (M + BM - 1) / BM, tn = (N + BN - 1) / BN;
     constexpr int MOST = 1 << 18;      // tiles of a launch, whose threads, one to eight values, are fewer than 2^32
     for (int t0 = 0; t0 < tm * tn; t0 += MOST) {
         const int n = tm * tn - t0 < MOST ? tm * tn - t0 : MOST;
         const TailSplit ts{part + (size_t)t0 * (BM * BN), t0, n, 1, 0};
         hipLaunchKernelGGL((tail_sum_kernel<BM, BN>), dim3(n * (BM * BN / 8 / 256)), dim3(256), 0, s, ts, M, N, tm, tn,
-                           (const __bf16 *)nullptr, (const __bf16 *)nullptr, 0, (__bf16 *)C, N, (const int32_t *)nullptr);
+                           (const __bf16 *)nullptr, (const __bf16 *)R, N, (__bf16 *)C, N, (const int32_t *)nullptr);
     }
 }
 void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, bool first, hipStream_t s) {
@@ -1237,11 +1279,11 @@ void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int
     else if (p.kind == SMALL) nn_piece<128, 128, 4>(M, N, K, A, lda, B, part, first, s);
     else nn_piece<64, 64, 8>(M, N, K, A, lda, B, part, first, s);
 }
-void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, hipStream_t s) {
-    ProfScope prof(K_REDUCE, s, 6.0 * M * N);
-    if (p.kind == BIG) nn_round<256, 256>(M, N, part, C, s);
-    else if (p.kind == SMALL) nn_round<128, 128>(M, N, part, C, s);
-    else nn_round<64, 64>(M, N, part, C, s);
+void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, const void *R, hipStream_t s) {
+    ProfScope prof(K_REDUCE, s, 8.0 * M * N);
+    if (p.kind == BIG) nn_round<256, 256>(M, N, part, C, R, s);
+    else if (p.kind == SMALL) nn_round<128, 128>(M, N, part, C, R, s);
+    else nn_round<64, 64>(M, N, part, C, R, s);
 }
 
 }  // namespace ob

@@ -79,8 +79,127 @@ __global__ __launch_bounds__(256) void rows_spread_kernel(const __bf16 *__restri
     }
 }
 
+// The label's entry of a row of G is most of that row of dx and, with the others of its label, of a row of dw: rounded to bf16 it scales them by up to 2^-8, all
+// of them alike where the weights are (dnll of 1 / 1020 for every row: dx and dw 0.0042 off, 0.0017 with this).  So what its rounding took, `lack` in fp32, goes into
+// the products' epilogues: dx[r] = lack_r W[label], the residual of G W, and for the first row r of every label own[r] = sum of lack x over its rows (r, then the others
+// in order), which the epilogue of G^T x finds by lead[column] = r.  bf16 will do for both, 2^-8 of what is lost.
+// A workgroup to a row; it looks for an earlier row of its label first.  Bound by the labels that it reads out of the L2, n times the fewer of n and V (8185 rows, 131072 x
+// 6144: 126 us of the step's 35.7 ms; 3271 rows, 65536 x 4096: 31 of 5.2; 40000 rows, 50000 x 1024: 0.79 of 16), and by the first row of a label that many share,
+// whose workgroup adds them all up (4 % of those 8185 rows one label: 0.2 ms more, 30 %: 1.3).
+constexpr int LABEL_SCAN = 2048, LABEL_VECS = 4;      // (LABEL_VECS vectors of 8 columns to a thread: rows of up to 8192)
+__global__ __launch_bounds__(256) void loss_labels_kernel(int n, int H, int V, int first, int cols, const float *__restrict__ lack, int32_t *__restrict__ lead,
+                                                          const int32_t *__restrict__ labels, const __bf16 *__restrict__ x, const __bf16 *__restrict__ w,
+                                                          __bf16 *__restrict__ dx, __bf16 *__restrict__ own) {
+    constexpr int PER = LABEL_SCAN / 256, AHEAD = 8;
+    __shared__ uint64_t mask[PER][4];
+    __shared__ int list[LABEL_SCAN];
+    __shared__ float sums[256][8];
+    const int r = blockIdx.x, label = labels[r], tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // narrow rows: `groups` of threads take rows in turns
+    const int span = min(256, H / 8), groups = 256 / span, group = tid / span, c0 = (tid - group * span) * 8;
+    if (label < 0 || label >= V) {
+        if (first == 0 && group == 0)
+            for (int c = c0; c < H; c += 2048) *(bf16x8 *)(dx + (size_t)r * H + c) = bf16x8{};
+        return;
+    }
+    if (label < first || label - first >= cols) return;
+    const float mine = lack[r];
+    if (group == 0)
+        for (int c = c0; c < H; c += 2048) {
+            const bf16x8 v = *(const bf16x8 *)(w + (size_t)(label - first) * H + c);
+            bf16x8 o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = (__bf16)(mine * (float)v[e]);
+            *(bf16x8 *)(dx + (size_t)r * H + c) = o;
+        }
+    for (int i0 = 0; i0 < r; i0 += 2 * LABEL_SCAN) {
+        int same = 0;
+#pragma unroll
+        for (int k = 0; k < 2 * PER; ++k) {
+            const int i = i0 + k * 256 + tid;
+            same |= labels[min(i, r)] == label && i < r;
+        }
+        if (__syncthreads_or(same)) return;
+    }
+    float acc[LABEL_VECS][8] = {};
+    for (int i0 = r; i0 < n; i0 += LABEL_SCAN) {
+        bool hit[PER];
+        int any = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int i = i0 + k * 256 + tid;
+            hit[k] = labels[min(i, n - 1)] == label && i < n;
+            any |= hit[k];
+        }
+        if (!__syncthreads_or(any)) continue;  // (also: the list of the rows before is done with)
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const uint64_t m = __ballot(hit[k]);
+            if (lane == 0) mask[k][wave] = m;
+        }
+        __syncthreads();
+        int count = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const uint64_t m = mask[k][v];
+                if (v == wave && hit[k]) list[count + __popcll(m & ((1ull << lane) - 1))] = i0 + k * 256 + tid;
+                count += __popcll(m);
+            }
+        __syncthreads();
+        // the rows in turns of the groups, AHEAD of them on their way
+#pragma unroll
+        for (int vec = 0; vec < LABEL_VECS; ++vec) {
+            const int c = c0 + vec * 2048;
+            if (c >= H || group >= groups) break;
+            for (int at = group; at < count; at += groups * AHEAD) {
+                bf16x8 v[AHEAD];
+                float f[AHEAD];
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a) {
+                    const int row = list[min(at + a * groups, count - 1)];
+                    f[a] = lack[row];
+                    v[a] = *(const bf16x8 *)(x + (size_t)row * H + c);
+                }
+#pragma unroll
+                for (int a = 0; a < AHEAD; ++a)
+                    if (at + a * groups < count) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) acc[vec][e] += f[a] * (float)v[a][e];
+                    }
+            }
+        }
+    }
+    if (groups > 1) {                          // (one vector to a thread)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[tid][e] = acc[0][e];
+        __syncthreads();
+        if (group != 0) return;
+        for (int g = 1; g < groups; ++g)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[0][e] += sums[g * span + tid][e];
+    }
+#pragma unroll
+    for (int vec = 0; vec < LABEL_VECS; ++vec) {
+        const int c = c0 + vec * 2048;
+        if (c >= H) break;
+        bf16x8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = (__bf16)acc[vec][e];
+        *(bf16x8 *)(own + (size_t)r * H + c) = o;
+    }
+    if (tid == 0) lead[label - first] = r;
+}
+
 }  // namespace
 
+void launch_loss_labels(int n, int H, int V, int first, int cols, const float *lack, int32_t *lead, const int32_t *labels, const void *x, const void *w,
+                        void *dx, void *own, hipStream_t s) {
+    ProfScope prof(K_ROWS, s, 8.0 * n * H);
+    hipLaunchKernelGGL(loss_labels_kernel, dim3(n), dim3(256), 0, s, n, H, V, first, cols, lack, lead, labels, (const __bf16 *)x, (const __bf16 *)w, (__bf16 *)dx,
+                       (__bf16 *)own);
+}
 void launch_loss_combine(const void *stats, const float *target, const int32_t *labels, int n, int V, int slots, float *nll, float *lse,
                          hipStream_t s) {
     ProfScope prof(K_REDUCE, s, 8.0 * n * slots);

@@ -33,7 +33,7 @@ struct Pieces {
 
 int slots_of(const Plan &p, int V) { return 2 * ((V + tile_cols(p.kind) - 1) / tile_cols(p.kind)); }
 
-struct Work { size_t xs, stats, target, g, dxs, sums, sums_bytes, total; };
+struct Work { size_t xs, stats, target, g, dxs, own, sums, sums_bytes, total; };
 Work work_layout(int n, int V, int H) {
     const Plan logits = whole_plan(0, n, V, H);
     const Pieces pc(n, V);
@@ -44,7 +44,8 @@ Work work_layout(int n, int V, int H) {
     w.stats = fwd.take((size_t)slots_of(logits, V) * n * 8);
     w.target = fwd.take((size_t)n * 4);
     w.dxs = bwd.take((size_t)n * H * 2);
-    w.g = bwd.take((size_t)n * pc.ld * 2);
+    w.own = bwd.take((size_t)n * H * 2);
+    w.g = bwd.take(loss_grad_bytes(n, pc.ld));
     if (pc.count > 1) {
         const Plan p = whole_plan(1, n, H, pc.cols);
         w.sums_bytes = (size_t)p.n_full * tile_rows(p.kind) * tile_cols(p.kind) * 4;
@@ -169,7 +170,8 @@ extern "C" int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void
         xs = at + wk.xs;
         dxs = at + wk.dxs;
     }
-    // Per piece of the vocabulary: G = (softmax - one-hot) weight, its logits computed again; dW rows of the piece = G^T x, whole; dx += G W
+    // Per piece of the vocabulary: G = (softmax - one-hot) weight, its logits computed again; what its rounding took of the entries at the labels, which are
+    // most of a row of dx and of the labels' rows of dw; dW rows of the piece = G^T x, whole; dx += G W
     const Plan p_dx = whole_plan(1, n, H, pc.cols);
     float *sums = (float *)(at + wk.sums);
     unsigned char *g = at + wk.g;
@@ -178,11 +180,12 @@ extern "C" int ob_lm_loss_bwd(const ob_lm_loss_desc *desc, int flags, const void
         const unsigned char *wp = (const unsigned char *)w + (size_t)v0 * H * 2;
         unsigned char *dwp = (unsigned char *)dw + (size_t)v0 * H * 2;
         launch_loss_grad(whole_plan(0, n, cols, H), n, cols, H, xs, wp, labels, V, lse, dnll, v0, g, ld, s);
-        launch_gemm_tn(cols, H, n, g, ld, xs, dwp, acc ? dwp : nullptr, s);
+        launch_loss_labels(n, H, V, v0, cols, loss_lack(g, n, ld), loss_lead(g, n, ld), labels, xs, wp, dxs, at + wk.own, s);
+        launch_loss_dw(cols, H, n, g, ld, xs, dwp, acc ? dwp : nullptr, at + wk.own, s);
         if (pc.count > 1) launch_gemm_nn_piece(p_dx, n, H, cols, g, ld, wp, sums, i == 0, s);
-        else launch_gemm_nn(n, H, cols, g, ld, wp, dxs, wk.sums_bytes ? sums : nullptr, wk.sums_bytes, s);
+        else launch_gemm_nn(n, H, cols, g, ld, wp, dxs, dxs, wk.sums_bytes ? sums : nullptr, wk.sums_bytes, s);
     }
-    if (pc.count > 1) launch_gemm_nn_round(p_dx, n, H, sums, dxs, s);
+    if (pc.count > 1) launch_gemm_nn_round(p_dx, n, H, sums, dxs, dxs, s);
     if (rows_dev) launch_rows_spread(dxs, dx, rows_dev, n, total_tokens, H, s);
     return check_launch(who);
 }

@@ -61,15 +61,24 @@ struct Plan;
 void launch_loss_stats(const Plan &p, int n, int V, int H, const void *x, const void *w, const int32_t *labels, void *stats, float *target,
                        hipStream_t s);
 // g [n, ldg]: the gradient of the logits of `cols` of the V columns, `first` the first one's label, w its row of weights; ldg = cols up to a
-// multiple of 64
+// multiple of 64.  Behind it (loss_grad_bytes() in all) what the rows' entries at their labels lost in their rounding, and of each column, -1 or the first
+// row of its label
 void launch_loss_grad(const Plan &p, int n, int cols, int H, const void *x, const void *w, const int32_t *labels, int V, const float *lse,
                       const float *dnll, int first, void *g, int ldg, hipStream_t s);
-// C [M, N] = A [M, K] (row stride lda, zeros from K to a multiple of 64) B [K, N]; C = A [K, M]^T B [K, N] (+ R)
-void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *B, void *C, void *ws, size_t ws_bytes, hipStream_t s);
-void launch_gemm_tn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *R, hipStream_t s);
-// the first over pieces of K; part: whole tiles of p in fp32
+__host__ __device__ inline float *loss_lack(const void *g, int n, int ldg) { return (float *)((unsigned char *)g + (size_t)n * ldg * 2); }
+__host__ __device__ inline int32_t *loss_lead(const void *g, int n, int ldg) { return (int32_t *)(loss_lack(g, n, ldg) + n); }
+inline size_t loss_grad_bytes(int n, int ldg) { return (size_t)n * ldg * 2 + (size_t)n * 4 + (size_t)ldg * 4; }
+// gives both products what the rounding of the entries at the labels of this piece took: dx [n, H] = lack w[label] (0 for a row without a label, with the first
+// piece), own [n, H] row r the sum of lack x over the rows of r's label, if r is the first of them, and lead[column] = r
+void launch_loss_labels(int n, int H, int V, int first, int cols, const float *lack, int32_t *lead, const int32_t *labels, const void *x, const void *w,
+                        void *dx, void *own, hipStream_t s);
+// C [M, N] = A [M, K] (row stride lda, zeros from K to a multiple of 64) B [K, N] (+ R)
+void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *R, void *ws, size_t ws_bytes, hipStream_t s);
+// dw [M, N] = G [K, M]^T x [K, N] (+ R), with the rows of `own` where they belong
+void launch_loss_dw(int M, int N, int K, const void *G, int ldg, const void *x, void *dw, const void *R, const void *own, hipStream_t s);
+// "NN" over pieces of K; part: whole tiles of p in fp32
 void launch_gemm_nn_piece(const Plan &p, int M, int N, int K, const void *A, int lda, const void *B, float *part, bool first, hipStream_t s);
-void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, hipStream_t s);
+void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, const void *R, hipStream_t s);
 // stats of `slots` parts of the vocabulary and the labels' logits -> lse, nll (0 for a row without a label)
 void launch_loss_combine(const void *stats, const float *target, const int32_t *labels, int n, int V, int slots, float *nll, float *lse,
                          hipStream_t s);

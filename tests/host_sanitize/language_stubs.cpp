@@ -32,7 +32,7 @@ void see(const void *p, size_t bytes, int mark, const char *what) {
         std::abort();
     }
 }
-enum { XS = 1, STATS, TARGET, G, SUMS, DXS, DELTA, LSE2, PART };
+enum { XS = 1, STATS, TARGET, G, LACK, LEAD, OWN, SUMS, DXS, DELTA, LSE2, PART };
 int xs_mark = 0;       // rows gathered: they have to be there for every product; 0: the caller's x itself
 size_t slots(const ob::Plan &p, int V) { return 2 * (size_t)((V + ob::tile_cols(p.kind) - 1) / ob::tile_cols(p.kind)); }
 size_t sums_of(const ob::Plan &p) { return (size_t)p.n_full * ob::tile_rows(p.kind) * ob::tile_cols(p.kind) * 4; }
@@ -60,16 +60,29 @@ void launch_loss_grad(const Plan &, int n, int cols, int H, const void *x, const
     if (ldg < cols || ldg % 64 || ldg - cols >= 64) std::abort();
     see(x, (size_t)n * H * 2, xs_mark, "xs");
     put(g, (size_t)n * ldg * 2, G);
+    put(loss_lack(g, n, ldg), (size_t)n * 4, LACK);
+    put(loss_lead(g, n, ldg), (size_t)ldg * 4, LEAD);
 }
-void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *, void *C, void *ws, size_t ws_bytes, hipStream_t) {
+void launch_loss_labels(int n, int H, int, int, int cols, const float *lack, int32_t *lead, const int32_t *, const void *x, const void *, void *dx, void *own, hipStream_t) {
+    reach("launch_loss_labels");
+    see(lack, (size_t)n * 4, LACK, "lack");
+    see(lead, (size_t)cols * 4, LEAD, "lead");
+    see(x, (size_t)n * H * 2, xs_mark, "xs");
+    put(dx, (size_t)n * H * 2, DXS);
+    put(own, (size_t)n * H * 2, OWN);
+}
+void launch_gemm_nn(int M, int N, int K, const void *A, int lda, const void *, void *C, const void *R, void *ws, size_t ws_bytes, hipStream_t) {
     reach("launch_gemm_nn");
     if (ws) put(ws, ws_bytes, SUMS);
+    see(R, (size_t)M * N * 2, DXS, "dx's residual");
     if (ws && ws_bytes < gemm_workspace_bytes(1, M, N, K)) std::abort();
     see(A, (size_t)M * lda * 2, G, "g");
     put(C, (size_t)M * N * 2, DXS);
 }
-void launch_gemm_tn(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *, hipStream_t) {
-    reach("launch_gemm_tn");
+void launch_loss_dw(int M, int N, int K, const void *A, int lda, const void *B, void *C, const void *, const void *own, hipStream_t) {
+    reach("launch_loss_dw");
+    see(own, (size_t)K * N * 2, OWN, "own");
+    see(loss_lead(A, K, lda), (size_t)M * 4, LEAD, "lead");
     see(A, (size_t)K * lda * 2, G, "g");
     see(B, (size_t)K * N * 2, xs_mark, "xs");
     put(C, (size_t)M * N * 2, 0);
@@ -80,8 +93,9 @@ void launch_gemm_nn_piece(const Plan &p, int M, int, int, const void *A, int lda
     if (!first) see(part, sums_of(p), SUMS, "dx's sums");
     put(part, sums_of(p), SUMS);
 }
-void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, hipStream_t) {
+void launch_gemm_nn_round(const Plan &p, int M, int N, float *part, void *C, const void *R, hipStream_t) {
     reach("launch_gemm_nn_round");
+    see(R, (size_t)M * N * 2, DXS, "dx's residual");
     see(part, sums_of(p), SUMS, "dx's sums");
     put(C, (size_t)M * N * 2, DXS);
 }
