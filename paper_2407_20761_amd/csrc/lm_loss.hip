@@ -175,11 +175,11 @@ __global__ __launch_bounds__(256) void loss_labels_kernel(int n, int H, int V, i
 #pragma unroll
         for (int e = 0; e < 8; ++e) sums[tid][e] = acc[0][e];
         __syncthreads();
-        if (group != 0) return;
-        for (int g = 1; g < groups; ++g)
+        for (int g = 1; g < groups && group == 0; ++g)
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[0][e] += sums[g * span + tid][e];
     }
+    if (group != 0) return;                    // (threads of no group among them)
 #pragma unroll
     for (int vec = 0; vec < LABEL_VECS; ++vec) {
         const int c = c0 + vec * 2048;

@@ -46,7 +46,7 @@ def _check(c):
         assert _off(got, value) <= _factor(c, n) * float(torch.hypot(_off(_bf16(value), value, False), err)) + 3e-5 * float(value.norm()), n
 
 
-SIZES = [(60, 256, 32003), (990, 768, 32003), (4800, 512, 1009), (2100, 1024, 16384), (300, 64, 7), (5, 128, 100)]
+SIZES = [(60, 256, 32003), (990, 768, 32003), (4800, 512, 1009), (2100, 1024, 16384), (300, 64, 7), (5, 128, 100), (700, 1088, 900)]
 
 
 @gpu
@@ -80,7 +80,7 @@ def _labels(kind, n, V):
 
 @gpu
 @pytest.mark.parametrize("kind", ["one", "two", "runs", "far", "most"])
-@pytest.mark.parametrize("n,H,V", [(1, 64, 9), (257, 1024, 50), (4500, 192, 3000), (2049, 2112, 64)])
+@pytest.mark.parametrize("n,H,V", [(1, 64, 9), (257, 1024, 50), (4500, 192, 3000), (2049, 2112, 64), (1, 1088, 300), (600, 1088, 40), (300, 1984, 9), (300, 4160, 20), (40, 8192, 9)])
 def test_rows_of_one_label(n, H, V, kind):
     c = Call(n, H, V, seed=7)
     c.labels = _labels(kind, n, V).to(DEV).int()
