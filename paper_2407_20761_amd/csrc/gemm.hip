@@ -734,6 +734,10 @@ __device__ __forceinline__ void gemm_tile(
         }
         return;
     }
+    if constexpr (EPI == EPI_LOSS_DW) {      // the list's entries of the wave's rows, behind its slab
+        static_assert(32 * RSTR + BM / WM * 4 <= 4 * C::SLOT / C::NW, "wave's LDS share");
+        for (int i = lane; i < BM / WM; i += 64) ((int OB_LDS *)(slab + 32 * RSTR))[i] = loss_lead(A, K, lda)[min(m0 + wm * (BM / WM) + i, M - 1)];
+    }
     float cs[2][8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) cs[0][e] = cs[1][e] = 0.f;
@@ -751,11 +755,6 @@ __device__ __forceinline__ void gemm_tile(
         // take those (16400 x 3200 x 3200, NT: 285 us with the loads pair by pair, 265, 252 without a residual; weight gradient
         // 9600 x 3200 over 3075 rows, accumulated: 166, 151, 145).  Registers of the K loop's fragments hold them.
         bf16x8 res[MODE == 1 ? TA / 2 : 1][NR];
-        int OB_LDS *const lead = (int OB_LDS *)(slab + 32 * RSTR);      // (EPI_LOSS_DW) of the wave's rows
-        if constexpr (EPI == EPI_LOSS_DW) {
-            static_assert(32 * RSTR + BM / WM * 4 <= 4 * C::SLOT / C::NW, "behind the slab");
-            for (int i = lane; i < BM / WM; i += 64) lead[i] = loss_lead(A, K, lda)[min(m0 + wm * (BM / WM) + i, M - 1)];
-        }
         if constexpr (MODE == 1) {
 #pragma unroll
             for (int ii = 0; ii < TA / 2; ++ii)
@@ -781,7 +780,7 @@ __device__ __forceinline__ void gemm_tile(
             if constexpr (EPI == EPI_LOSS_DW) {
 #pragma unroll
                 for (int r = 0; r < NR; ++r) {
-                    const int row = lead[ii * 32 + r * RPI + lane / LPR];
+                    const int row = ((const int OB_LDS *)(slab + 32 * RSTR))[ii * 32 + r * RPI + lane / LPR];
                     r8[r] = bf16x8{};
                     if (row >= 0 && n_out < N) r8[r] = *(const bf16x8 *)(bias + (size_t)row * N + n_out);
                 }
