@@ -298,11 +298,12 @@ typedef struct {
     int dtype;         /* ob_dtype */
 } ob_lm_loss_desc;
 size_t ob_lm_loss_workspace_bytes(const ob_lm_loss_desc *desc, int n_rows);
-/* Host only, for tests: the tiles (rows, as many columns) of the bf16 launches over the logits, and of dx's sums over the pieces of the vocabulary. */
+/* Host only, for tests: the tiles (rows, as many columns) of the bf16 launches over the logits, of dx's sums over the pieces of the vocabulary, and of dw. */
 typedef struct {
     int fwd_tile, fwd_workgroups;
     int pieces, piece_tile, last_tile;      /* backward: pieces, tiles of the logits of one and of the last */
     int dx_tile;                            /* 0: one piece, an ordinary product */
+    int dw_tile;                            /* of a piece */
 } ob_lm_loss_launch;
 int ob_lm_loss_plan(const ob_lm_loss_desc *desc, int n_rows, ob_lm_loss_launch *launch);
 int ob_lm_loss_fwd(const ob_lm_loss_desc *desc, const void *w, const void *x, int total_tokens, const int32_t *rows_host,

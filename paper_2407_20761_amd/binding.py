@@ -65,7 +65,7 @@ class ob_lm_loss_desc(C.Structure):
 
 
 class ob_lm_loss_launch(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("fwd_tile", "fwd_workgroups", "pieces", "piece_tile", "last_tile", "dx_tile")]
+    _fields_ = [(n, C.c_int) for n in ("fwd_tile", "fwd_workgroups", "pieces", "piece_tile", "last_tile", "dx_tile", "dw_tile")]
 
 
 class ob_rotary_axes_desc(C.Structure):

@@ -1243,7 +1243,7 @@ static void loss_dw(int M, int N, int K, const void *G, int ldg, const void *x, 
 }
 void launch_loss_dw(int M, int N, int K, const void *G, int ldg, const void *x, void *dw, const void *R, const void *own, hipStream_t s) {
     ProfScope prof(K_GEMM, s, 2.0 * M * N * K);
-    const TileKind kind = make_row_cut(2, M, N, K, 0).rest.kind;
+    const TileKind kind = loss_dw_kind(M, N, K);
     if (kind == BIG) loss_dw<256, 4>(M, N, K, G, ldg, x, dw, R, own, s);
     else if (kind == SMALL) loss_dw<128, 4>(M, N, K, G, ldg, x, dw, R, own, s);
     else loss_dw<64, 8>(M, N, K, G, ldg, x, dw, R, own, s);

@@ -36,6 +36,8 @@ size_t scratch_bytes(int M, int N, int K);
 RowCut make_row_cut(int layout, int M, int N, int K, size_t scratch);
 // whole tiles, one launch, of one of three kinds: BIG, SMALL or FINE
 Plan whole_plan(int layout, int M, int N, int K);
+// the loss' dW ("TN") in one launch of whole tiles: the kind that a GEMM without scratch has
+inline TileKind loss_dw_kind(int M, int N, int K) { return make_row_cut(2, M, N, K, 0).rest.kind; }
 // GEMMs with an activation in the epilogue: layouts of gemm_any() beyond the three (internal).  Whether such a launch is taken instead of two, and its
 // plan; `scratch`: the GEMM alone would have room for slice sums
 enum { GEMM_NT_GELU = 3, GEMM_NN_GELU_BWD = 4, GEMM_NN_SWIGLU_BWD = 5 };

@@ -110,7 +110,8 @@ extern "C" int ob_lm_loss_plan(const ob_lm_loss_desc *desc, int n_rows, ob_lm_lo
     const Pieces pc(n, V);
     const Plan fwd = whole_plan(0, n, V, H), piece = whole_plan(0, n, pc.cols, H), last = whole_plan(0, n, V - (pc.count - 1) * pc.cols, H);
     *launch = ob_lm_loss_launch{tile_rows(fwd.kind), fwd.n_full, pc.count, tile_rows(piece.kind), tile_rows(last.kind),
-                                pc.count > 1 ? tile_rows(whole_plan(1, n, H, pc.cols).kind) : 0};
+                                pc.count > 1 ? tile_rows(whole_plan(1, n, H, pc.cols).kind) : 0,
+                                tile_rows(loss_dw_kind(pc.cols, H, n))};
     return OB_OK;
 }
 

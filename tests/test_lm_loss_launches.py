@@ -16,17 +16,18 @@ def _plan(n, H, V):
 
 # ---- every kind of tile ------------------------------------------------------------------------------
 
-# (rows, all tokens, hidden, vocabulary) -> tiles of the forward's logits, pieces, tiles of the logits of a piece, of the last, of dx's sums
+# (rows, all tokens, hidden, vocabulary) -> tiles of the forward's logits, pieces, tiles of the logits of a piece, of the last, of dx's sums, of dw
 LAUNCHES = [
-    ((2100, 2100, 1024, 16384), (256, 1, 256, 256, 0)),           # whole columns of tiles, ragged rows
-    ((2060, 5000, 1024, 16385), (256, 1, 256, 256, 0)),           # ragged both ways, listed rows
-    ((2049, 2049, 4096, 8200), (256, 1, 256, 256, 0)),
-    ((2100, 2100, 256, 16384), (128, 1, 128, 128, 0)),
-    ((257, 300, 768, 2001), (64, 1, 64, 64, 0)),
-    ((4100, 4100, 64, 131080), (128, 2, 128, 128, 64)),
-    ((4100, 4200, 1024, 131080), (256, 2, 256, 256, 128)),
-    ((4100, 4100, 2048, 131080), (256, 2, 256, 256, 256)),
-    ((9000, 9000, 1024, 120001), (256, 3, 256, 256, 256)),        # the sums of three pieces
+    ((2100, 2100, 1024, 16384), (256, 1, 256, 256, 0, 256)),           # whole columns of tiles, ragged rows
+    ((2060, 5000, 1024, 16385), (256, 1, 256, 256, 0, 128)),           # ragged both ways, listed rows
+    ((2049, 2049, 4096, 8200), (256, 1, 256, 256, 0, 128)),
+    ((2100, 2100, 256, 16384), (128, 1, 128, 128, 0, 128)),
+    ((257, 300, 768, 2001), (64, 1, 64, 64, 0, 128)),
+    ((4100, 4100, 64, 131080), (128, 2, 128, 128, 64, 128)),
+    ((4100, 4200, 1024, 131080), (256, 2, 256, 256, 128, 256)),
+    ((4100, 4100, 2048, 131080), (256, 2, 256, 256, 256, 256)),
+    ((9000, 9000, 1024, 120001), (256, 3, 256, 256, 256, 256)),        # the sums of three pieces
+    ((4800, 4800, 512, 1009), (128, 1, 128, 128, 0, 64)),
 ]
 
 
@@ -34,7 +35,7 @@ LAUNCHES = [
 def test_which_launches_a_case_takes(sizes, want):
     n, _, H, V = sizes
     p = _plan(n, H, V)
-    assert (p.fwd_tile, p.pieces, p.piece_tile, p.last_tile, p.dx_tile) == want
+    assert (p.fwd_tile, p.pieces, p.piece_tile, p.last_tile, p.dx_tile, p.dw_tile) == want
 
 
 @gpu

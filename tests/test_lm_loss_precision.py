@@ -97,10 +97,11 @@ def test_rows_of_one_label(n, H, V, kind):
 
 
 @gpu
-@pytest.mark.parametrize("n,H,V", [(990, 768, 3200), (2100, 1024, 16384)])
-def test_accumulated(n, H, V):
+@pytest.mark.parametrize("n,H,V,tile", [(4800, 512, 1009, 64), (990, 768, 3200, 128), (2100, 1024, 16384, 256)])
+def test_accumulated(n, H, V, tile):
     """the sum with what was there is rounded once: off by that and by G's roundings beside the labels"""
     c = Call(n, H, V, seed=5)
+    assert ob.ob_lm_loss_plan(c.desc, n).dw_tile == tile
     c.dnll.fill_(1 / 1020)
     old = (torch.randn(c.dw.shape, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV) * 1e-3).bfloat16()
     c.fwd()
